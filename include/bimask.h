@@ -14,8 +14,9 @@
  *     bimask_compress_nm       W_b   = compressed (Bbar .* W[P,:])^T             operand of Eq. (10)
  *     bimask_sparse_gemm_bwd   dX    = dY[:,P] * (Bbar .* W[P,:])                Eq. (10) / Eq. (8)
  *
- * The weight gradient dW = dY^T * X stays dense (straight-through estimator, Sec. 3.1)
- * and is not part of this library.
+ * The weight gradient dW = dY^T * X stays dense (straight-through estimator, Sec. 3.1); bimask_weight_grad
+ * takes it from an 8-bit checkpoint of X.  Around the products: bimask_sparse_linear_fwd (bias, activation,
+ * residual), bimask_act_bwd, bimask_checkpoint_store / _load.
  *
  * Shapes and layouts (all row-major, zero-based; "ld" = leading dimension in elements):
  *     W      I x J   weights, I = out features, J = in features          (Sec. 3.1)
@@ -104,8 +105,14 @@ typedef enum { BIMASK_F32 = 0, BIMASK_BF16 = 1 } bimask_dtype;
 typedef enum {
     BIMASK_WS_PERM_SEARCH = 0,
     BIMASK_WS_GEMM_FWD = 1,
-    BIMASK_WS_GEMM_BWD = 2
+    BIMASK_WS_GEMM_BWD = 2,
+    BIMASK_WS_ACT_BWD = 3,      /* I, T */
+    BIMASK_WS_WEIGHT_GRAD = 4   /* I, J, T, dtype */
 } bimask_ws_kind;
+
+/* Activations: z; max(z, 0) (slope 0 at 0); z Phi(z) with the normal distribution function Phi; its tanh approximation
+ * z / 2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))); z / (1 + exp(-z)). */
+typedef enum { BIMASK_ACT_NONE = 0, BIMASK_ACT_RELU = 1, BIMASK_ACT_GELU = 2, BIMASK_ACT_GELU_TANH = 3, BIMASK_ACT_SILU = 4 } bimask_act;
 
 /* Forward mask, Eq. (4) under the constraint of Eq. (2): in every group of M consecutive
  * columns of every row keep the N largest magnitudes.
@@ -204,6 +211,55 @@ BIMASK_API int bimask_sparse_gemm_bwd(const void *dY, int64_t T, int64_t lddy, c
                            int dtype, int N, int M, void *dX, int64_t lddx,
                            void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- The layer around the product: epilogue, 8-bit activation checkpoints, their use in the backward pass ----
+ *
+ * Checkpoint of a T x C matrix (bimask_checkpoint_bytes(T, C) bytes, 16-byte aligned): T rows of codes, one signed byte per
+ * feature, the row padded with zero codes to Cp = C rounded up to 32; then, from byte T * Cp on, T rows of Cp/32 scale bytes.  32
+ * consecutive features of a token share a power of two 2^e, e the smallest with rint(max|x| / 2^e) <= 127, kept within -126 <= e <=
+ * 121; the scale byte is e + 127, a code is rint(x / 2^e) (halves to even) within +-127, and the pair stands for code * 2^e: off by
+ * at most half of 2^e (less than 2^e where e was kept to 121, magnitudes from 127.5 * 2^121 on).  A block that holds an infinity or NaN has the scale byte 255 and
+ * codes 0 and stands for 32 NaN.  The values are exact in both dtypes, and codes depend on the inputs alone.
+ *
+ * Errors of these calls are those of the others; in addition BIMASK_ERR_WORKSPACE for a checkpoint buffer smaller than
+ * bimask_checkpoint_bytes says, BIMASK_ERR_UNSUPPORTED for an activation that does not exist and for outputs that overlap inputs
+ * other than as stated.  T, C >= 1 (these matrices need not be multiples of M); pointers aligned to their elements unless stated;
+ * rows that start on 16 bytes take the fast path. */
+BIMASK_API size_t bimask_checkpoint_bytes(int64_t T, int64_t C);
+
+/* X (T x C, ldx >= C, dtype) -> checkpoint, and back (X out: the values the checkpoint stands for). */
+BIMASK_API int bimask_checkpoint_store(const void *X, int64_t T, int64_t C, int64_t ldx, int dtype, void *ckpt, size_t ckpt_bytes,
+                            void *stream);
+BIMASK_API int bimask_checkpoint_load(const void *ckpt, size_t ckpt_bytes, int64_t T, int64_t C, int dtype, void *X, int64_t ldx,
+                           void *stream);
+
+/* Forward product with its epilogue:  Z = X (B .* W)^T + bias,  Y = act(Z) + residual.
+ * Operands, layouts and alignments of bimask_sparse_gemm_fwd; sums, activation and residual in fp32, one rounding at the end.
+ *   bias      in   I entries of dtype, 16-byte aligned, or NULL
+ *   residual  in   T x I (ldr >= I; bf16: 4-byte aligned, even ldr) or NULL; may be Y itself (same pointer and leading dimension)
+ *   ckpt      out  checkpoint of Z (T x I), from its fp32 values, or NULL                                                   */
+BIMASK_API int bimask_sparse_linear_fwd(const void *X, int64_t T, int64_t ldx, const void *Wf_values, const uint32_t *Wf_index,
+                             int64_t I, int64_t J, int dtype, int N, int M, const void *bias, int act, const void *residual,
+                             int64_t ldr, void *Y, int64_t ldy, void *ckpt, size_t ckpt_bytes, void *stream);
+
+/* Backward of the activation and the bias:  dZ = dY * act'(Z~),  dbias[i] = sum_t dZ[t][i], Z~ the values of Z's checkpoint.
+ *   dY      in   T x I (lddy >= I), dtype
+ *   ckpt    in   checkpoint of Z (T x I); may be NULL with BIMASK_ACT_NONE
+ *   dZ      out  T x I (lddz >= I), dtype, or NULL; may be dY itself (same pointer and leading dimension)
+ *   dbias   out  I fp32, or NULL; summed in fp32 before dZ is rounded, in an order that depends on T and I alone
+ *   workspace  bimask_workspace_bytes(BIMASK_WS_ACT_BWD, I, 0, T, ...) bytes, 16-byte aligned; not used without dbias          */
+BIMASK_API int bimask_act_bwd(const void *dY, int64_t T, int64_t lddy, const void *ckpt, size_t ckpt_bytes, int64_t I, int dtype, int act,
+                   void *dZ, int64_t lddz, float *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Weight gradient of the straight-through estimator (Sec. 3.1), dense:  dW[i][j] = sum_t dY[t][i] X~[t][j], X~ the values of X's
+ * checkpoint; fp32 sums in an order that depends on the sizes alone.
+ *   dY    in   T x I (lddy >= I), dtype
+ *   ckpt  in   checkpoint of X (T x J)
+ *   dW    out  I x J (lddw >= J), dw_dtype: BIMASK_F32, or BIMASK_BF16 with bf16 dY; accumulate = 1: added to what dW holds
+ *   workspace  bimask_workspace_bytes(BIMASK_WS_WEIGHT_GRAD, I, J, T, 0, dtype, ...) bytes, 16-byte aligned                   */
+BIMASK_API int bimask_weight_grad(const void *dY, int64_t T, int64_t lddy, const void *ckpt, size_t ckpt_bytes, int64_t I, int64_t J,
+                       int dtype, void *dW, int64_t lddw, int dw_dtype, int accumulate, void *workspace, size_t workspace_bytes,
+                       void *stream);
+
 /* Debug helper, off the hot path: the search, the backward mask, the backward GEMM and the
  * refinement trust that what they are given are permutations of 0 .. I-1 (Sec. 3.3: P is a row
  * permutation) and read rows through them unchecked.  This call checks K candidates:
@@ -279,7 +335,7 @@ BIMASK_API int bimask_perm_refine_group(const bimask_group_layer *layers, int n,
 BIMASK_API int64_t bimask_operand_elems(int64_t rows, int64_t cols, int N, int M);
 BIMASK_API int64_t bimask_operand_index_words(int64_t rows, int64_t cols, int N, int M);
 
-/* Scratch bytes a call needs (0 if none).  kind is a bimask_ws_kind.                     */
+/* Scratch bytes a call needs (0 if none).  kind is a bimask_ws_kind; arguments that its comment does not name are ignored. */
 BIMASK_API size_t bimask_workspace_bytes(int kind, int64_t I, int64_t J, int64_t T, int K, int dtype, int N, int M);
 
 /* Static, never NULL.                                                                    */

@@ -13,7 +13,9 @@ import os
 from typing import Optional, Tuple
 
 F32, BF16 = 0, 1
-WS_PERM_SEARCH, WS_GEMM_FWD, WS_GEMM_BWD = 0, 1, 2
+WS_PERM_SEARCH, WS_GEMM_FWD, WS_GEMM_BWD, WS_ACT_BWD, WS_WEIGHT_GRAD = 0, 1, 2, 3, 4
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
+ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH, "silu": ACT_SILU}
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libbimask.so")
@@ -36,6 +38,12 @@ _SIGNATURES = {
     "bimask_perm_search_group": (_INT, [_PTR, _INT, _INT, _INT, _INT, _PTR]),
     "bimask_backward_mask_compress_group": (_INT, [_PTR, _INT, _INT, _INT, _INT, _PTR]),
     "bimask_perm_refine_group": (_INT, [_PTR, _INT, _INT, _INT, _PTR]),
+    "bimask_checkpoint_bytes": (_SZ, [_I64, _I64]),
+    "bimask_checkpoint_store": (_INT, [_PTR, _I64, _I64, _I64, _INT, _PTR, _SZ, _PTR]),
+    "bimask_checkpoint_load": (_INT, [_PTR, _SZ, _I64, _I64, _INT, _PTR, _I64, _PTR]),
+    "bimask_sparse_linear_fwd": (_INT, [_PTR, _I64, _I64, _PTR, _PTR, _I64, _I64, _INT, _INT, _INT, _PTR, _INT, _PTR, _I64, _PTR, _I64, _PTR, _SZ, _PTR]),
+    "bimask_act_bwd": (_INT, [_PTR, _I64, _I64, _PTR, _SZ, _I64, _INT, _INT, _PTR, _I64, _PTR, _PTR, _SZ, _PTR]),
+    "bimask_weight_grad": (_INT, [_PTR, _I64, _I64, _PTR, _SZ, _I64, _I64, _INT, _PTR, _I64, _INT, _INT, _PTR, _SZ, _PTR]),
     "bimask_operand_elems": (_I64, [_I64, _I64, _INT, _INT]),
     "bimask_operand_index_words": (_I64, [_I64, _I64, _INT, _INT]),
     "bimask_workspace_bytes": (_SZ, [_INT, _I64, _I64, _I64, _INT, _INT, _INT, _INT]),
@@ -369,6 +377,145 @@ def bimask_sparse_gemm_bwd(dY, perm, Wb_values, Wb_index, I: int, J: int, N: int
            lib().bimask_sparse_gemm_bwd(_ptr(dY), T, lddy, _ptr(perm), _ptr(Wb_values), _ptr(Wb_index), I, J,
                                         _dtype_code(dY), N, M, _ptr(dX), lddx, _ptr(workspace), wsb, _stream()))
     return dX
+
+
+# -- the layer around the product: epilogue, 8-bit checkpoints, gradients ------------------------------
+def checkpoint_bytes(T: int, cols: int) -> int:
+    return int(lib().bimask_checkpoint_bytes(T, cols))
+
+
+def _on_current_device(*ts):
+    """The calls below enqueue on the current device's stream: tensors of another device are refused."""
+    _need_cuda(*ts)
+    if _device_index is None:
+        _bind_stream()
+    d = _device_index()
+    for t in ts:
+        if t is not None and t.get_device() != d:
+            raise ValueError("all tensors must live on the current device")
+
+
+def _pitch(t) -> int:
+    """Leading dimension of a matrix with unit stride along its rows; of a single row it is no stride that anyone steps by."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] != 1):
+        raise ValueError("expected a 2-D tensor with unit stride along its last dimension")
+    return t.stride(0) if t.shape[0] != 1 else (t.shape[1] + 7) // 8 * 8
+
+
+def _expect(t, name: str, shape, dtype) -> None:
+    if t is not None and (tuple(t.shape) != shape or t.dtype != dtype):
+        raise ValueError(f"{name} must be a {' x '.join(map(str, shape))} tensor of {dtype}")
+
+
+def _ckpt_buffer(ckpt, T: int, cols: int, like):
+    import torch
+    if ckpt is None:
+        return _empty((checkpoint_bytes(T, cols),), torch.uint8, like)
+    if ckpt.dtype != torch.uint8 or not ckpt.is_contiguous():
+        raise ValueError("a checkpoint is a contiguous uint8 tensor")
+    return ckpt
+
+
+def _workspace(workspace, need: int, like):
+    if workspace is None and need:
+        import torch
+        return _empty((need,), torch.uint8, like)
+    return workspace
+
+
+def bimask_checkpoint_store(X, ckpt=None):
+    """The 8-bit checkpoint of X, T x C: a uint8 tensor of checkpoint_bytes(T, C) bytes."""
+    _on_current_device(X, ckpt)
+    ldx = _pitch(X)
+    T, C = X.shape
+    ckpt = _ckpt_buffer(ckpt, T, C, X)
+    _check("bimask_checkpoint_store",
+           lib().bimask_checkpoint_store(_ptr(X), T, C, ldx, _dtype_code(X), _ptr(ckpt), _nbytes(ckpt), _stream()))
+    return ckpt
+
+
+def bimask_checkpoint_load(ckpt, T: int, C: int, dtype=None, X=None):
+    """The values that a checkpoint stands for, T x C in `dtype` (torch.bfloat16 if neither it nor X says otherwise)."""
+    import torch
+    _on_current_device(ckpt, X)
+    _ckpt_buffer(ckpt, T, C, ckpt)
+    if X is None:
+        X = _empty((T, C), dtype or torch.bfloat16, ckpt)
+    _expect(X, "X", (T, C), dtype or X.dtype)
+    _check("bimask_checkpoint_load",
+           lib().bimask_checkpoint_load(_ptr(ckpt), _nbytes(ckpt), T, C, _dtype_code(X), _ptr(X), _pitch(X), _stream()))
+    return X
+
+
+def bimask_sparse_linear_fwd(X, Wf_values, Wf_index, I: int, J: int, N: int, M: int, bias=None, act: int = ACT_NONE, residual=None,
+                             Y=None, ckpt=None, want_ckpt: bool = False):
+    """Y = act(Z) + residual with Z = X (B .* W)^T + bias; returns (Y, checkpoint of Z or None).  residual may be Y itself."""
+    _on_current_device(X, Wf_values, Wf_index, bias, residual, Y, ckpt)
+    ldx = _pitch(X)
+    T = X.shape[0]
+    _expect(X, "X", (T, J), X.dtype)
+    if Wf_values.dtype != X.dtype or Wf_values.numel() < operand_elems(I, J, N, M):
+        raise ValueError("Wf_values must hold the operand of an I x J matrix in the type of X")
+    if Wf_index is not None and Wf_index.numel() < operand_index_words(I, J, N, M):
+        raise ValueError("Wf_index must hold the index words of an I x J matrix")
+    _expect(bias, "bias", (I,), X.dtype)
+    if bias is not None and not bias.is_contiguous():
+        raise ValueError("bias must be contiguous")
+    _expect(residual, "residual", (T, I), X.dtype)
+    if Y is None:
+        Y = _empty((T, I), None, X)
+    _expect(Y, "Y", (T, I), X.dtype)
+    if want_ckpt or ckpt is not None:
+        ckpt = _ckpt_buffer(ckpt, T, I, X)
+    _check("bimask_sparse_linear_fwd",
+           lib().bimask_sparse_linear_fwd(_ptr(X), T, ldx, _ptr(Wf_values), _ptr(Wf_index), I, J, _dtype_code(X), N, M, _ptr(bias), act,
+                                          _ptr(residual), 0 if residual is None else _pitch(residual), _ptr(Y), _pitch(Y), _ptr(ckpt),
+                                          _nbytes(ckpt), _stream()))
+    return Y, ckpt
+
+
+def bimask_act_bwd(dY, ckpt, act: int, dZ=None, dbias=None, want_dZ: bool = True, want_dbias: bool = True, workspace=None):
+    """(dZ, dbias): dZ = dY * act'(Z) with Z from its checkpoint (None with ACT_NONE), dbias its column sums in fp32; either is None
+    if not wanted.  dZ may be dY itself."""
+    import torch
+    _on_current_device(dY, ckpt, dZ, dbias, workspace)
+    lddy = _pitch(dY)
+    T, I = dY.shape
+    if ckpt is not None:
+        _ckpt_buffer(ckpt, T, I, ckpt)
+    if dZ is None and want_dZ:
+        dZ = _empty((T, I), None, dY)
+    _expect(dZ, "dZ", (T, I), dY.dtype)
+    if dbias is None and want_dbias:
+        dbias = _empty((I,), torch.float32, dY)
+    _expect(dbias, "dbias", (I,), torch.float32)
+    if dbias is not None:
+        if not dbias.is_contiguous():
+            raise ValueError("dbias must be contiguous")
+        workspace = _workspace(workspace, workspace_bytes(WS_ACT_BWD, I, 0, T, 0, _dtype_code(dY), 0, 0), dY)
+    _check("bimask_act_bwd",
+           lib().bimask_act_bwd(_ptr(dY), T, lddy, _ptr(ckpt), _nbytes(ckpt), I, _dtype_code(dY), act, _ptr(dZ),
+                                0 if dZ is None else _pitch(dZ), _ptr(dbias), _ptr(workspace), _nbytes(workspace), _stream()))
+    return dZ, dbias
+
+
+def bimask_weight_grad(dY, ckpt, J: int, dW=None, dw_dtype=None, accumulate: bool = False, workspace=None):
+    """dW = dY^T X (I x J, dense) with X (T x J) from its checkpoint; in `dw_dtype` (that of dY if neither it nor dW says otherwise);
+    accumulate: added to what dW holds."""
+    _on_current_device(dY, ckpt, dW, workspace)
+    lddy = _pitch(dY)
+    T, I = dY.shape
+    _ckpt_buffer(ckpt, T, J, ckpt)
+    if dW is None:
+        if accumulate:
+            raise ValueError("accumulate needs a dW to add to")
+        dW = _empty((I, J), dw_dtype, dY)
+    _expect(dW, "dW", (I, J), dw_dtype or dW.dtype)
+    workspace = _workspace(workspace, workspace_bytes(WS_WEIGHT_GRAD, I, J, T, 0, _dtype_code(dY), 0, 0), dY)
+    _check("bimask_weight_grad",
+           lib().bimask_weight_grad(_ptr(dY), T, lddy, _ptr(ckpt), _nbytes(ckpt), I, J, _dtype_code(dY), _ptr(dW), _pitch(dW),
+                                    _dtype_code(dW), int(bool(accumulate)), _ptr(workspace), _nbytes(workspace), _stream()))
+    return dW
 
 
 # -- grouped calls: the mask / search steps of several independent layers in a few launches -------

@@ -1,0 +1,120 @@
+// Activations, their slopes and the 8-bit checkpoint's block rule (see include/bimask.h), for kernels that apply them to
+// fp32 values in registers.
+#pragma once
+#include "common.hpp"
+
+namespace bimask {
+
+// ---- activations ------------------------------------------------------------------------------------------------
+// silu and gelu_tanh are one family, z * sigma(u) with u = z (c1 + c2 z^2): sigma by one exponential of -|u|, so nothing
+// overflows and 1 - sigma keeps its digits.  gelu is z * Phi(z) with Phi's tail 0.5 erfc(|z| / sqrt 2) = exp(-z^2 / 2) R(|z|);
+// R (the Mills ratio over sqrt(2 pi)) as t * polynomial(t), t = 1 / (1 + 0.3 |z|): least squares on the relative error,
+// re-weighted to equal peaks, 1.5e-7 over 0 <= |z| <= 14.  The tail itself never comes from 1 - Phi.
+// (What 2^x and 1/x cost: a quarter of the rate of an addition each; two of them and about 14 other operations an element.)
+struct ActCoef { float c1, c2; };
+__host__ __device__ inline ActCoef act_coef(int act) {
+    return act == BIMASK_ACT_SILU ? ActCoef{1.f, 0.f} : ActCoef{1.5957691216f, 0.0713548163f};      // 2 sqrt(2/pi), times 0.044715
+}
+
+struct Sigma { float s, d; };                            // sigma(u) and sigma'(u)
+__device__ __forceinline__ Sigma sigma(float u) {
+    const float e = __builtin_amdgcn_exp2f(-1.44269504f * __builtin_fabsf(u));
+    const float r = __builtin_amdgcn_rcpf(1.f + e), er = e * r;
+    return {u >= 0.f ? r : er, er * r};
+}
+__device__ __forceinline__ float sigma_arg(float z, const ActCoef& c) { return z * (c.c1 + c.c2 * __builtin_fminf(z * z, 1e30f)); }
+
+__device__ __forceinline__ float gauss(float z) { return __builtin_amdgcn_exp2f(-0.721347520f * z * z); }       // exp(-z^2 / 2)
+__device__ __forceinline__ float phi_cdf(float z, float g) {
+    const float t = __builtin_amdgcn_rcpf(1.f + 0.3f * __builtin_fabsf(z));
+    float p = 0.03567478f;
+    p = __builtin_fmaf(p, t, -0.1572031f);
+    p = __builtin_fmaf(p, t, 0.20635354f);
+    p = __builtin_fmaf(p, t, -0.05368367f);
+    p = __builtin_fmaf(p, t, 0.12856164f);
+    p = __builtin_fmaf(p, t, 0.09991349f);
+    p = __builtin_fmaf(p, t, 0.12075396f);
+    p = __builtin_fmaf(p, t, 0.1196293f);
+    const float tail = g * (t * p);
+    return z >= 0.f ? 1.f - tail : tail;
+}
+
+// z -> act(z), for n values; act is uniform
+template <int n>
+__device__ __forceinline__ void apply_act(float (&z)[n], int act) {
+    if (act == BIMASK_ACT_NONE) return;
+    if (act == BIMASK_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) z[i] = z[i] <= 0.f ? 0.f : z[i];         // (NaN stays)
+    } else if (act == BIMASK_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) z[i] *= phi_cdf(z[i], gauss(z[i]));
+    } else {
+        const ActCoef c = act_coef(act);
+#pragma unroll
+        for (int i = 0; i < n; ++i) z[i] *= sigma(sigma_arg(z[i], c)).s;
+    }
+}
+
+// z -> act'(z); z is finite or NaN (a checkpoint's values are).  relu: 0 at 0.
+template <int n>
+__device__ __forceinline__ void apply_slope(float (&z)[n], int act) {
+    if (act == BIMASK_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) z[i] = 1.f;
+    } else if (act == BIMASK_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) z[i] = z[i] <= 0.f ? 0.f : z[i] > 0.f ? 1.f : z[i];
+    } else if (act == BIMASK_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float g = gauss(z[i]);
+            z[i] = __builtin_fmaf(z[i], 0.398942280f * g, phi_cdf(z[i], g));
+        }
+    } else {
+        const ActCoef c = act_coef(act);
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const Sigma s = sigma(sigma_arg(z[i], c));
+            // sigma' is 0 long before the polynomial leaves the range, where 0 * inf would be NaN
+            z[i] = __builtin_fmaf(z[i] * s.d, __builtin_fmaf(3.f * c.c2, __builtin_fminf(z[i] * z[i], 1e30f), c.c1), s.s);
+        }
+    }
+}
+
+// ---- 8-bit checkpoints --------------------------------------------------------------------------------------------
+// 32 consecutive features of a token share a power of two 2^e, the smallest with rint(max / 2^e) <= 127; every product with
+// 2^e or 2^-e is exact, so codes depend on the inputs alone and the values they stand for are exact in bf16 and fp32.
+constexpr int kCkptBlock = 32;
+__host__ __device__ inline int64_t ckpt_pitch(int64_t cols) { return round_up(cols, kCkptBlock); }      // bytes of codes per token
+__host__ __device__ inline int64_t ckpt_blocks(int64_t cols) { return ceil_div(cols, kCkptBlock); }     // scale bytes per token
+
+constexpr int64_t kMaxTokens = int64_t(1) << 38;         // rows of the matrices around the product: sizes in bytes stay in 64 bits
+constexpr int kCkptNaN = 255;
+// The scale byte e + 127 of a block whose largest magnitude has these bits (sign cleared; a NaN orders above infinity).  127.5 is
+// 1.9921875 * 2^6, mantissa bits 0x7F0000: from there on the next power.  -126 <= e <= 121 keeps 2^e, 2^-e and 127 * 2^e normal.
+__device__ __forceinline__ int ckpt_scale_byte(uint32_t most) {
+    const int x = static_cast<int>(most >> 23);
+    if (x == 255) return kCkptNaN;
+    const int b = x - 6 + ((most & 0x7FFFFFu) >= 0x7F0000u ? 1 : 0);
+    return b < 1 ? 1 : b > 248 ? 248 : b;
+}
+__device__ __forceinline__ float ckpt_inverse(int byte) { return __builtin_bit_cast(float, static_cast<uint32_t>(254 - byte) << 23); }
+__device__ __forceinline__ float ckpt_scale(int byte) {
+    return __builtin_bit_cast(float, byte == kCkptNaN ? 0x7FC00000u : static_cast<uint32_t>(byte) << 23);
+}
+// 4 values -> 4 codes, first in the low byte; `inv` 0 for a block that reads as NaN (its codes are written as 0)
+__device__ __forceinline__ uint32_t ckpt_codes(const float* v, float inv, bool bad) {
+    uint32_t r = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float q = __builtin_fminf(__builtin_fmaxf(__builtin_rintf(v[i] * inv), -127.f), 127.f);
+        r |= (static_cast<uint32_t>(static_cast<int>(q)) & 0xFFu) << (8 * i);
+    }
+    return bad ? 0u : r;
+}
+__device__ __forceinline__ float ckpt_value(uint32_t four, int i, float scale) {      // code i of 4
+    return static_cast<float>(static_cast<int8_t>(four >> (8 * i))) * scale;
+}
+
+}  // namespace bimask

@@ -1,6 +1,6 @@
 // extern "C" boundary of the Bi-Mask library: argument validation on the host, then
 // kernel launches on the caller's stream.  See include/bimask.h for the contract.
-#include "common.hpp"
+#include "act.hpp"
 
 using namespace bimask;
 
@@ -47,6 +47,36 @@ int check_gemm(const void* act, int64_t T, int64_t ldact, int64_t kdim, const vo
     }
     return BIMASK_OK;
 }
+
+int check_act(int act) { return act >= BIMASK_ACT_NONE && act <= BIMASK_ACT_SILU ? BIMASK_OK : BIMASK_ERR_UNSUPPORTED; }
+
+bool aligned_elem(const void* p, int dtype) { return reinterpret_cast<uintptr_t>(p) % esize(dtype) == 0; }
+
+// rows * pitch in bytes stays within 64 bits
+bool sizes_fit(int64_t T, int64_t ld) {
+    int64_t n;
+    return !__builtin_mul_overflow(T, ld, &n) && n <= (int64_t(1) << 56);
+}
+
+// A T x C matrix of the calls around the product (no multiple of M needed).
+int check_rows(const void* p, int64_t T, int64_t C, int64_t ld, int dtype) {
+    if (!p) return BIMASK_ERR_NULL;
+    if (int rc = check_dtype(dtype)) return rc;
+    if (T <= 0 || C <= 0 || T > kMaxTokens || C > 0x7FFFFFFFll || ld < C || !sizes_fit(T, ld)) return BIMASK_ERR_SHAPE;
+    return aligned_elem(p, dtype) ? BIMASK_OK : BIMASK_ERR_ALIGN;
+}
+
+int check_ckpt(const void* ckpt, size_t bytes, int64_t T, int64_t C) {
+    if (!ckpt) return BIMASK_ERR_NULL;
+    if (bytes < bimask_checkpoint_bytes(T, C)) return BIMASK_ERR_WORKSPACE;
+    return aligned16(ckpt) ? BIMASK_OK : BIMASK_ERR_ALIGN;
+}
+
+bool apart(const void* a, size_t abytes, const void* b, size_t bbytes) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x + abytes <= y || y + bbytes <= x;
+}
+size_t span(int64_t T, int64_t ld, int64_t C, int dtype) { return static_cast<size_t>((T - 1) * ld + C) * esize(dtype); }
 
 }  // namespace
 
@@ -256,6 +286,87 @@ int bimask_sparse_gemm_bwd(const void* dY, int64_t T, int64_t lddy, const int32_
     return launch_gemm(Wb_values, Wb_index, J, I, sp, act, T, ldact, dX, lddx, dtype, as_stream(stream));
 }
 
+size_t bimask_checkpoint_bytes(int64_t T, int64_t C) {
+    if (T <= 0 || C <= 0 || T > kMaxTokens || C > 0x7FFFFFFFll) return 0;
+    return static_cast<size_t>(T) * static_cast<size_t>(ckpt_pitch(C) + ckpt_blocks(C));
+}
+
+int bimask_checkpoint_store(const void* X, int64_t T, int64_t C, int64_t ldx, int dtype, void* ckpt, size_t ckpt_bytes, void* stream) {
+    if (int rc = check_rows(X, T, C, ldx, dtype)) return rc;
+    if (int rc = check_ckpt(ckpt, ckpt_bytes, T, C)) return rc;
+    if (!apart(X, span(T, ldx, C, dtype), ckpt, bimask_checkpoint_bytes(T, C))) return BIMASK_ERR_UNSUPPORTED;
+    return launch_checkpoint_store(X, T, C, ldx, dtype, static_cast<uint8_t*>(ckpt), as_stream(stream));
+}
+
+int bimask_checkpoint_load(const void* ckpt, size_t ckpt_bytes, int64_t T, int64_t C, int dtype, void* X, int64_t ldx, void* stream) {
+    if (int rc = check_rows(X, T, C, ldx, dtype)) return rc;
+    if (int rc = check_ckpt(ckpt, ckpt_bytes, T, C)) return rc;
+    if (!apart(X, span(T, ldx, C, dtype), ckpt, bimask_checkpoint_bytes(T, C))) return BIMASK_ERR_UNSUPPORTED;
+    return launch_checkpoint_load(static_cast<const uint8_t*>(ckpt), T, C, dtype, X, ldx, as_stream(stream));
+}
+
+int bimask_sparse_linear_fwd(const void* X, int64_t T, int64_t ldx, const void* Wf_values, const uint32_t* Wf_index, int64_t I, int64_t J,
+                             int dtype, int N, int M, const void* bias, int act, const void* residual, int64_t ldr, void* Y, int64_t ldy,
+                             void* ckpt, size_t ckpt_bytes, void* stream) {
+    if (int rc = check_gemm(X, T, ldx, J, Wf_values, Wf_index, I, J, dtype, N, M, Y, ldy, I)) return rc;
+    if (T > kMaxTokens || I > 0x7FFFFFFFll || J > 0x7FFFFFFFll || !sizes_fit(T, ldx) || !sizes_fit(T, ldy)) return BIMASK_ERR_SHAPE;
+    if (int rc = check_act(act)) return rc;
+    if (bias && !aligned16(bias)) return BIMASK_ERR_ALIGN;
+    if (residual) {
+        if (ldr < I || !sizes_fit(T, ldr)) return BIMASK_ERR_SHAPE;
+        if (!aligned4(residual) || (dtype == BIMASK_BF16 && ldr % 2)) return BIMASK_ERR_ALIGN;
+        if (!(residual == Y && ldr == ldy) && !disjoint(residual, T, ldr, I, Y, ldy, I, esize(dtype))) return BIMASK_ERR_UNSUPPORTED;
+    }
+    if (!disjoint(X, T, ldx, J, Y, ldy, I, esize(dtype))) return BIMASK_ERR_UNSUPPORTED;
+    if (ckpt) {
+        if (int rc = check_ckpt(ckpt, ckpt_bytes, T, I)) return rc;
+        const size_t need = bimask_checkpoint_bytes(T, I);
+        if (!apart(ckpt, need, X, span(T, ldx, J, dtype)) || !apart(ckpt, need, Y, span(T, ldy, I, dtype)) ||
+            (residual && !apart(ckpt, need, residual, span(T, ldr, I, dtype)))) return BIMASK_ERR_UNSUPPORTED;
+    }
+    return launch_linear(Wf_values, Wf_index, I, J, uses_sp24(N, M), X, T, ldx, dtype, bias, act, residual, ldr, Y, ldy,
+                         static_cast<uint8_t*>(ckpt), as_stream(stream));
+}
+
+int bimask_act_bwd(const void* dY, int64_t T, int64_t lddy, const void* ckpt, size_t ckpt_bytes, int64_t I, int dtype, int act, void* dZ,
+                   int64_t lddz, float* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = check_rows(dY, T, I, lddy, dtype)) return rc;
+    if (int rc = check_act(act)) return rc;
+    if (!dZ && !dbias) return BIMASK_ERR_NULL;
+    if (ckpt || act != BIMASK_ACT_NONE)
+        if (int rc = check_ckpt(ckpt, ckpt_bytes, T, I)) return rc;
+    const size_t need = bimask_checkpoint_bytes(T, I);
+    if (dZ) {
+        if (int rc = check_rows(dZ, T, I, lddz, dtype)) return rc;
+        if (!(dZ == dY && lddz == lddy) && !disjoint(dY, T, lddy, I, dZ, lddz, I, esize(dtype))) return BIMASK_ERR_UNSUPPORTED;
+        if (ckpt && !apart(ckpt, need, dZ, span(T, lddz, I, dtype))) return BIMASK_ERR_UNSUPPORTED;
+    }
+    if (dbias) {
+        if (!aligned4(dbias)) return BIMASK_ERR_ALIGN;
+        const size_t ws = plan_act_bwd(T, I).ws_bytes;
+        if (ws > 0 && (!workspace || workspace_bytes < ws)) return BIMASK_ERR_WORKSPACE;
+        if (ws > 0 && !aligned16(workspace)) return BIMASK_ERR_ALIGN;
+    }
+    return launch_act_bwd(dY, T, lddy, act == BIMASK_ACT_NONE ? nullptr : static_cast<const uint8_t*>(ckpt), I, dtype, act, dZ, lddz, dbias,
+                          static_cast<float*>(workspace), as_stream(stream));
+}
+
+int bimask_weight_grad(const void* dY, int64_t T, int64_t lddy, const void* ckpt, size_t ckpt_bytes, int64_t I, int64_t J, int dtype, void* dW,
+                       int64_t lddw, int dw_dtype, int accumulate, void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = check_rows(dY, T, I, lddy, dtype)) return rc;
+    if (int rc = check_rows(dW, I, J, lddw, dw_dtype)) return rc;
+    if (dtype == BIMASK_F32 && dw_dtype != BIMASK_F32) return BIMASK_ERR_DTYPE;
+    if (accumulate != 0 && accumulate != 1) return BIMASK_ERR_UNSUPPORTED;
+    if (int rc = check_ckpt(ckpt, ckpt_bytes, T, J)) return rc;
+    const size_t out = span(I, lddw, J, dw_dtype);
+    if (!apart(dW, out, dY, span(T, lddy, I, dtype)) || !apart(dW, out, ckpt, bimask_checkpoint_bytes(T, J))) return BIMASK_ERR_UNSUPPORTED;
+    const size_t ws = plan_weight_grad(T, I, J, dtype).ws_bytes;
+    if (ws > 0 && (!workspace || workspace_bytes < ws)) return BIMASK_ERR_WORKSPACE;
+    if (ws > 0 && !aligned16(workspace)) return BIMASK_ERR_ALIGN;
+    return launch_weight_grad(dY, T, lddy, static_cast<const uint8_t*>(ckpt), I, J, dtype, dW, lddw, dw_dtype, accumulate == 1,
+                              static_cast<float*>(workspace), as_stream(stream));
+}
+
 int64_t bimask_operand_elems(int64_t rows, int64_t cols, int N, int M) {
     if (rows <= 0 || cols <= 0) return 0;
     if (uses_sp24(N, M)) return round_up(rows, 32) * (round_up(cols, 128) / 2);
@@ -269,8 +380,12 @@ int64_t bimask_operand_index_words(int64_t rows, int64_t cols, int N, int M) {
 
 size_t bimask_workspace_bytes(int kind, int64_t I, int64_t J, int64_t T, int K, int dtype, int N, int M) {
     (void)N; (void)M;
+    if (kind == BIMASK_WS_ACT_BWD) return I > 0 && T > 0 && I <= 0x7FFFFFFFll && T <= kMaxTokens ? plan_act_bwd(T, I).ws_bytes : 0;
     if (I <= 0 || J <= 0) return 0;
     switch (kind) {
+        case BIMASK_WS_WEIGHT_GRAD:
+            return T > 0 && T <= kMaxTokens && I <= 0x7FFFFFFFll && J <= 0x7FFFFFFFll && check_dtype(dtype) == BIMASK_OK
+                       ? plan_weight_grad(T, I, J, dtype).ws_bytes : 0;
         case BIMASK_WS_PERM_SEARCH: {
             if (K <= 0) return 0;
             if (M != 4 && M != 8 && M != 16) return 0;

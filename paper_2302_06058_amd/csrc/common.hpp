@@ -249,4 +249,33 @@ bool gemm_sp24_coltile_shape(int64_t Adim, int64_t K);
 // The same for dense masked weights (N > 2), which have no other fused path: 128 < K <= 2048, Adim <= min(K, 512).
 bool gemm_dense_coltile_shape(int64_t Adim, int64_t K);
 
+// 8-bit activation checkpoints, the gradient through an activation (checkpoint.hip)
+int launch_checkpoint_store(const void* X, int64_t T, int64_t J, int64_t ldx, int dtype, uint8_t* ckpt, hipStream_t s);
+int launch_checkpoint_load(const uint8_t* ckpt, int64_t T, int64_t J, int dtype, void* X, int64_t ldx, hipStream_t s);
+struct ActBwdPlan {
+    int log2c;           // threads side by side
+    int64_t tiles;       // feature tiles
+    int64_t rows;        // tokens of a strip
+    int64_t strips;
+    size_t ws_bytes;     // partial bias gradients of the strips
+};
+ActBwdPlan plan_act_bwd(int64_t T, int64_t I);
+int launch_act_bwd(const void* dY, int64_t T, int64_t lddy, const uint8_t* ckpt, int64_t I, int dtype, int act, void* dZ, int64_t lddz,
+                   float* dbias, float* ws, hipStream_t s);
+
+// Y = act(X (B .* W)^T + bias) + residual with an optional checkpoint of the pre-activation (linear.hip)
+int launch_linear(const void* A, const uint32_t* meta, int64_t Adim, int64_t K, bool sparse24, const void* Bm, int64_t T, int64_t ldb, int dtype,
+                  const void* bias, int act, const void* residual, int64_t ldr, void* C, int64_t ldc, uint8_t* ckpt, hipStream_t s);
+
+// dW = dY^T X~ from X's checkpoint (weight_grad.hip)
+struct WeightGradPlan {
+    bool big;            // 256 x 256 output tiles
+    int64_t rows;        // tokens of a piece
+    int64_t pieces;
+    size_t ws_bytes;     // sums of the pieces
+};
+WeightGradPlan plan_weight_grad(int64_t T, int64_t I, int64_t J, int dtype);
+int launch_weight_grad(const void* dY, int64_t T, int64_t lddy, const uint8_t* ckpt, int64_t I, int64_t J, int dtype, void* dW, int64_t lddw,
+                       int dw_dtype, bool accumulate, float* ws, hipStream_t s);
+
 }  // namespace bimask
