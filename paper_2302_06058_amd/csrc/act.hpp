@@ -6,23 +6,17 @@
 namespace bimask {
 
 // ---- activations ------------------------------------------------------------------------------------------------
-// silu and gelu_tanh are one family, z * sigma(u) with u = z (c1 + c2 z^2): sigma by one exponential of -|u|, so nothing
-// overflows and 1 - sigma keeps its digits.  gelu is z * Phi(z) with Phi's tail 0.5 erfc(|z| / sqrt 2) = exp(-z^2 / 2) R(|z|);
-// R (the Mills ratio over sqrt(2 pi)) as t * polynomial(t), t = 1 / (1 + 0.3 |z|): least squares on the relative error,
-// re-weighted to equal peaks, 1.5e-7 over 0 <= |z| <= 14.  The tail itself never comes from 1 - Phi.
-// (What 2^x and 1/x cost: a quarter of the rate of an addition each; two of them and about 14 other operations an element.)
-struct ActCoef { float c1, c2; };
-__host__ __device__ inline ActCoef act_coef(int act) {
-    return act == BIMASK_ACT_SILU ? ActCoef{1.f, 0.f} : ActCoef{1.5957691216f, 0.0713548163f};      // 2 sqrt(2/pi), times 0.044715
-}
+// silu and gelu_tanh are z * sigma(u), u = z and u = z (c1 + c2 z^2), sigma(u) = 1 / (1 + exp(-u)): an exponential that overflows
+// makes sigma 0, one that vanishes makes it 1.  Slopes as sigma + z sigma (1 - sigma) u', the product sigma (1 - sigma) first: it is
+// exactly 0 at both ends, where the other factors are finite.  gelu is z * Phi(z) with Phi's tail 0.5 erfc(|z| / sqrt 2) =
+// exp(-z^2 / 2) R(|z|); R (the Mills ratio over sqrt(2 pi)) as t * polynomial(t), t = 1 / (1 + 0.3 |z|): least squares on the
+// relative error, re-weighted to equal peaks, 1.5e-7 over 0 <= |z| <= 14.  The tail itself never comes from 1 - Phi.
+// Cost of a value in issue slots (2^x and 1/x take four each): silu 11, gelu_tanh 13, gelu 24; slopes 12, 17, 25.
+constexpr float kLog2e = 1.44269504f, kTanhC1 = 1.5957691216f, kTanhC2 = 0.0713548163f;       // 2 sqrt(2/pi), times 0.044715
 
-struct Sigma { float s, d; };                            // sigma(u) and sigma'(u)
-__device__ __forceinline__ Sigma sigma(float u) {
-    const float e = __builtin_amdgcn_exp2f(-1.44269504f * __builtin_fabsf(u));
-    const float r = __builtin_amdgcn_rcpf(1.f + e), er = e * r;
-    return {u >= 0.f ? r : er, er * r};
+__device__ __forceinline__ float sigma_of(float minus_u_log2e) {
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(minus_u_log2e));
 }
-__device__ __forceinline__ float sigma_arg(float z, const ActCoef& c) { return z * (c.c1 + c.c2 * __builtin_fminf(z * z, 1e30f)); }
 
 __device__ __forceinline__ float gauss(float z) { return __builtin_amdgcn_exp2f(-0.721347520f * z * z); }       // exp(-z^2 / 2)
 __device__ __forceinline__ float phi_cdf(float z, float g) {
@@ -49,10 +43,12 @@ __device__ __forceinline__ void apply_act(float (&z)[n], int act) {
     } else if (act == BIMASK_ACT_GELU) {
 #pragma unroll
         for (int i = 0; i < n; ++i) z[i] *= phi_cdf(z[i], gauss(z[i]));
-    } else {
-        const ActCoef c = act_coef(act);
+    } else if (act == BIMASK_ACT_SILU) {
 #pragma unroll
-        for (int i = 0; i < n; ++i) z[i] *= sigma(sigma_arg(z[i], c)).s;
+        for (int i = 0; i < n; ++i) z[i] *= sigma_of(-kLog2e * z[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < n; ++i) z[i] *= sigma_of(z[i] * __builtin_fmaf(-kLog2e * kTanhC2, z[i] * z[i], -kLog2e * kTanhC1));
     }
 }
 
@@ -71,13 +67,18 @@ __device__ __forceinline__ void apply_slope(float (&z)[n], int act) {
             const float g = gauss(z[i]);
             z[i] = __builtin_fmaf(z[i], 0.398942280f * g, phi_cdf(z[i], g));
         }
-    } else {
-        const ActCoef c = act_coef(act);
+    } else if (act == BIMASK_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < n; ++i) {
-            const Sigma s = sigma(sigma_arg(z[i], c));
-            // sigma' is 0 long before the polynomial leaves the range, where 0 * inf would be NaN
-            z[i] = __builtin_fmaf(z[i] * s.d, __builtin_fmaf(3.f * c.c2, __builtin_fminf(z[i] * z[i], 1e30f), c.c1), s.s);
+            const float s = sigma_of(-kLog2e * z[i]);
+            z[i] = __builtin_fmaf(z[i], __builtin_fmaf(-s, s, s), s);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float zz = __builtin_fminf(z[i] * z[i], 1e4f);         // (sigma is 0 or 1 long before; z^2 and u' stay finite)
+            const float s = sigma_of(z[i] * __builtin_fmaf(-kLog2e * kTanhC2, zz, -kLog2e * kTanhC1));
+            z[i] = __builtin_fmaf(z[i] * __builtin_fmaf(-s, s, s), __builtin_fmaf(3.f * kTanhC2, zz, kTanhC1), s);
         }
     }
 }

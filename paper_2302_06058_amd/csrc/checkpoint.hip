@@ -11,6 +11,8 @@ namespace bimask {
 namespace {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef uint32_t u32_any __attribute__((aligned(2)));
 
 constexpr int kPiece = 16;                               // features of a thread: half a block of the checkpoint
 constexpr int64_t kMaxGroups = 1 << 20;                  // workgroups of a launch; more work runs in a loop (a launch counts its work-items in 32 bits)
@@ -36,34 +38,59 @@ struct Row16 {                                           // 16 features of a row
                 else v[p][d] = __builtin_bit_cast(uint32_t, f[4 * p + d]);
             }
     }
-    // features c .. c + 15 of a row of `cols`; `whole`: rows start on 16 bytes
-    __device__ __forceinline__ void load(const raw* row, int64_t c, int64_t cols, bool whole) {
-        if (whole && c + kPiece <= cols) {
+    // features c .. c + 15 of a row of `cols`, rows at any element's alignment (the 16-byte accesses need no more); the end of a
+    // row in smaller pieces
+    __device__ __forceinline__ void load(const raw* row, int64_t c, int64_t cols) {
+        constexpr int E = 16 / sizeof(raw);
+        row += c;
+        const int64_t n = cols - c;
+        if (n >= kPiece) {
 #pragma unroll
-            for (int p = 0; p < V; ++p) v[p] = reinterpret_cast<const u32x4*>(row + c)[p];
-        } else {
+            for (int p = 0; p < V; ++p) v[p] = reinterpret_cast<const u32x4_any*>(row)[p];
+            return;
+        }
 #pragma unroll
-            for (int p = 0; p < V; ++p) v[p] = (u32x4){0u, 0u, 0u, 0u};
+        for (int p = 0; p < V; ++p) {
+            v[p] = (u32x4){0u, 0u, 0u, 0u};
+            if (n >= E * (p + 1)) {
+                v[p] = reinterpret_cast<const u32x4_any*>(row)[p];
+            } else {
 #pragma unroll
-            for (int i = 0; i < kPiece; ++i)
-                if (c + i < cols) {
-                    const uint32_t x = row[c + i];
-                    if constexpr (sizeof(raw) == 2) v[i >> 3][(i >> 1) & 3] |= x << (16 * (i & 1));
-                    else v[i >> 2][i & 3] = x;
+                for (int d = 0; d < 4; ++d) {
+                    if constexpr (sizeof(raw) == 4) {
+                        if (E * p + d < n) v[p][d] = row[E * p + d];
+                    } else {
+                        if (E * p + 2 * d + 1 < n) v[p][d] = *reinterpret_cast<const u32_any*>(row + E * p + 2 * d);
+                        else if (E * p + 2 * d < n) v[p][d] = row[E * p + 2 * d];
+                    }
                 }
+            }
         }
     }
-    __device__ __forceinline__ void store(raw* row, int64_t c, int64_t cols, bool whole) const {
-        if (whole && c + kPiece <= cols) {
+    __device__ __forceinline__ void store(raw* row, int64_t c, int64_t cols) const {
+        constexpr int E = 16 / sizeof(raw);
+        row += c;
+        const int64_t n = cols - c;
+        if (n >= kPiece) {
 #pragma unroll
-            for (int p = 0; p < V; ++p) reinterpret_cast<u32x4*>(row + c)[p] = v[p];
-        } else {
+            for (int p = 0; p < V; ++p) reinterpret_cast<u32x4_any*>(row)[p] = v[p];
+            return;
+        }
 #pragma unroll
-            for (int i = 0; i < kPiece; ++i)
-                if (c + i < cols) {
-                    if constexpr (sizeof(raw) == 2) row[c + i] = static_cast<raw>(v[i >> 3][(i >> 1) & 3] >> (16 * (i & 1)));
-                    else row[c + i] = v[i >> 2][i & 3];
+        for (int p = 0; p < V; ++p) {
+            if (n >= E * (p + 1)) {
+                reinterpret_cast<u32x4_any*>(row)[p] = v[p];
+            } else {
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    if constexpr (sizeof(raw) == 4) {
+                        if (E * p + d < n) row[E * p + d] = v[p][d];
+                    } else {
+                        if (E * p + 2 * d + 1 < n) *reinterpret_cast<u32_any*>(row + E * p + 2 * d) = v[p][d];
+                        else if (E * p + 2 * d < n) row[E * p + 2 * d] = static_cast<raw>(v[p][d]);
+                    }
                 }
+            }
         }
     }
 };
@@ -79,13 +106,13 @@ __device__ __forceinline__ Piece piece_at(int64_t first, uint32_t per_row) {
 template <typename raw>
 __global__ void __launch_bounds__(kThreads)
 k_checkpoint_store(const raw* __restrict__ X, int64_t T, int64_t J, int64_t ldx, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
-                   uint32_t per_row, bool whole) {
+                   uint32_t per_row) {
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * kThreads; first < T * per_row; first += static_cast<int64_t>(gridDim.x) * kThreads) {
         const Piece p = piece_at(first, per_row);
         if (p.t >= T) return;                            // pieces come in pairs of lanes: a block is never cut
         const int64_t c = static_cast<int64_t>(p.half) * kPiece;
         Row16<raw> x;
-        x.load(X + p.t * ldx, c, J, whole);
+        x.load(X + p.t * ldx, c, J);
         float f[kPiece];
         uint32_t most = 0;
 #pragma unroll
@@ -108,7 +135,7 @@ k_checkpoint_store(const raw* __restrict__ X, int64_t T, int64_t J, int64_t ldx,
 template <typename raw>
 __global__ void __launch_bounds__(kThreads)
 k_checkpoint_load(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t T, int64_t J, raw* __restrict__ X,
-                  int64_t ldx, uint32_t per_row, bool whole) {
+                  int64_t ldx, uint32_t per_row) {
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * kThreads; first < T * per_row; first += static_cast<int64_t>(gridDim.x) * kThreads) {
         const Piece p = piece_at(first, per_row);
         if (p.t >= T) return;
@@ -119,7 +146,7 @@ k_checkpoint_load(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
         for (int i = 0; i < kPiece; ++i) f[i] = ckpt_value(q[i >> 2], i & 3, scale);
         Row16<raw> x;
         x.put(f);
-        x.store(X + p.t * ldx, static_cast<int64_t>(p.half) * kPiece, J, whole);
+        x.store(X + p.t * ldx, static_cast<int64_t>(p.half) * kPiece, J);
     }
 }
 
@@ -129,7 +156,7 @@ k_checkpoint_load(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
 template <typename raw>
 __global__ void __launch_bounds__(kThreads)
 k_act_bwd(const raw* dY, int64_t T, int64_t lddy, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t I, int act,
-          raw* dZ, int64_t lddz, float* __restrict__ sums, int64_t ld_sums, int64_t rows, uint32_t per_row, int log2c, bool whole_in, bool whole_out) {
+          raw* dZ, int64_t lddz, float* __restrict__ sums, int64_t ld_sums, int64_t rows, uint32_t per_row, int log2c) {
     __shared__ float part[kThreads][kPiece + 1];
     const uint32_t half = (blockIdx.x << log2c) + (threadIdx.x & ((1u << log2c) - 1));
     const int64_t c = static_cast<int64_t>(half) * kPiece, t0 = static_cast<int64_t>(blockIdx.y) * rows;
@@ -137,29 +164,46 @@ k_act_bwd(const raw* dY, int64_t T, int64_t lddy, const uint8_t* __restrict__ co
     float acc[kPiece];
 #pragma unroll
     for (int i = 0; i < kPiece; ++i) acc[i] = 0.f;
+    const int64_t step = kThreads >> log2c;
+    // U rows are requested before the first is used
+    constexpr int U = 2;
     if (c < I)
-        for (int64_t t = t0 + (threadIdx.x >> log2c); t < t_end; t += kThreads >> log2c) {
-            Row16<raw> x;
-            x.load(dY + t * lddy, c, I, whole_in);
-            float f[kPiece];
-            if (codes) {                                 // none with act none: the bias gradient alone
-                const u32x4 q = *reinterpret_cast<const u32x4*>(codes + (t * per_row + half) * kPiece);
-                const float scale = ckpt_scale(scales[t * (per_row / 2) + half / 2]);
+        for (int64_t tb = t0 + (threadIdx.x >> log2c); tb < t_end; tb += U * step) {
+            Row16<raw> x[U];
+            u32x4 q[U];
+            int byte[U];
 #pragma unroll
-                for (int i = 0; i < kPiece; ++i) f[i] = ckpt_value(q[i >> 2], i & 3, scale);
-                apply_slope(f, act);
-#pragma unroll
-                for (int i = 0; i < kPiece; ++i) f[i] *= x.get(i);
-            } else {
-#pragma unroll
-                for (int i = 0; i < kPiece; ++i) f[i] = x.get(i);
-            }
-            if (dZ) {
-                x.put(f);
-                x.store(dZ + t * lddz, c, I, whole_out);
+            for (int u = 0; u < U; ++u) {
+                const int64_t t = tb + u * step < t_end ? tb + u * step : tb;      // beyond the strip: loaded, not used
+                x[u].load(dY + t * lddy, c, I);
+                if (codes) {                             // none with act none: the bias gradient alone
+                    q[u] = *reinterpret_cast<const u32x4*>(codes + (t * per_row + half) * kPiece);
+                    byte[u] = scales[t * (per_row / 2) + half / 2];
+                }
             }
 #pragma unroll
-            for (int i = 0; i < kPiece; ++i) acc[i] += f[i];
+            for (int u = 0; u < U; ++u) {
+                const int64_t t = tb + u * step;
+                if (t >= t_end) break;
+                float f[kPiece];
+                if (codes) {
+                    const float scale = ckpt_scale(byte[u]);
+#pragma unroll
+                    for (int i = 0; i < kPiece; ++i) f[i] = ckpt_value(q[u][i >> 2], i & 3, scale);
+                    apply_slope(f, act);
+#pragma unroll
+                    for (int i = 0; i < kPiece; ++i) f[i] *= x[u].get(i);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kPiece; ++i) f[i] = x[u].get(i);
+                }
+                if (dZ) {
+                    x[u].put(f);
+                    x[u].store(dZ + t * lddz, c, I);
+                }
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i) acc[i] += f[i];
+            }
         }
     if (!sums) return;
 #pragma unroll
@@ -174,17 +218,25 @@ k_act_bwd(const raw* dY, int64_t T, int64_t lddy, const uint8_t* __restrict__ co
     }
 }
 
+// 16 features x 16 ranges of strips per workgroup: a chain of additions is strips / 16 long instead of strips (100 strips of 1000
+// features 24 us with one thread per feature), and both levels add in a fixed order.
 __global__ void __launch_bounds__(kThreads)
 k_sum_strips(const float* __restrict__ part, int strips, int64_t ld, int64_t I, float* __restrict__ out) {
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    if (c >= I) return;
+    __shared__ float sums[16][17];
+    const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * 16 + x;         // (strips are as wide as whole blocks: in bounds)
     float s = 0.f;
-    for (int k = 0; k < strips; ++k) s += part[k * ld + c];
-    out[c] = s;
+#pragma unroll 4
+    for (int k = y; k < strips; k += 16) s += part[k * ld + c];
+    sums[y][x] = s;
+    __syncthreads();
+    if (y == 0 && c < I) {
+        float t = 0.f;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) t += sums[k][x];
+        out[c] = t;
+    }
 }
-
-template <typename raw>
-bool whole_rows(const void* p, int64_t ld) { return aligned16(p) && (ld * sizeof(raw)) % 16 == 0; }
 
 unsigned groups(int64_t pieces) {
     const int64_t n = ceil_div(pieces, kThreads);
@@ -199,10 +251,10 @@ int launch_checkpoint_store(const void* X, int64_t T, int64_t J, int64_t ldx, in
     const dim3 grid(groups(T * per_row));
     if (dtype == BIMASK_BF16)
         hipLaunchKernelGGL(k_checkpoint_store<uint16_t>, grid, dim3(kThreads), 0, s, static_cast<const uint16_t*>(X), T, J, ldx, ckpt, scales,
-                           per_row, whole_rows<uint16_t>(X, ldx));
+                           per_row);
     else
         hipLaunchKernelGGL(k_checkpoint_store<uint32_t>, grid, dim3(kThreads), 0, s, static_cast<const uint32_t*>(X), T, J, ldx, ckpt, scales,
-                           per_row, whole_rows<uint32_t>(X, ldx));
+                           per_row);
     return check_launch();
 }
 
@@ -211,22 +263,20 @@ int launch_checkpoint_load(const uint8_t* ckpt, int64_t T, int64_t J, int dtype,
     const uint8_t* scales = ckpt + T * ckpt_pitch(J);
     const dim3 grid(groups(T * per_row));
     if (dtype == BIMASK_BF16)
-        hipLaunchKernelGGL(k_checkpoint_load<uint16_t>, grid, dim3(kThreads), 0, s, ckpt, scales, T, J, static_cast<uint16_t*>(X), ldx, per_row,
-                           whole_rows<uint16_t>(X, ldx));
+        hipLaunchKernelGGL(k_checkpoint_load<uint16_t>, grid, dim3(kThreads), 0, s, ckpt, scales, T, J, static_cast<uint16_t*>(X), ldx, per_row);
     else
-        hipLaunchKernelGGL(k_checkpoint_load<uint32_t>, grid, dim3(kThreads), 0, s, ckpt, scales, T, J, static_cast<uint32_t*>(X), ldx, per_row,
-                           whole_rows<uint32_t>(X, ldx));
+        hipLaunchKernelGGL(k_checkpoint_load<uint32_t>, grid, dim3(kThreads), 0, s, ckpt, scales, T, J, static_cast<uint32_t*>(X), ldx, per_row);
     return check_launch();
 }
 
 // Feature tiles of up to 256 (16 threads side by side, a row segment of 512 bytes of bf16), and strips of tokens so that about
-// 2048 workgroups exist, none with fewer than 4 steps.
+// 2048 workgroups exist, none with fewer than 2 steps (one request of loads).
 ActBwdPlan plan_act_bwd(int64_t T, int64_t I) {
     ActBwdPlan p;
     const int64_t per_row = ckpt_pitch(I) / kPiece;
     p.log2c = per_row >= 16 ? 4 : ilog2(static_cast<int>(per_row));
     p.tiles = ceil_div(per_row, int64_t(1) << p.log2c);
-    const int64_t step = kThreads >> p.log2c, most = ceil_div(T, 4 * step);
+    const int64_t step = kThreads >> p.log2c, most = ceil_div(T, 2 * step);
     int64_t strips = ceil_div(2048, p.tiles);
     strips = strips < most ? strips : most;
     p.rows = round_up(ceil_div(T, strips), step);
@@ -246,15 +296,13 @@ int launch_act_bwd(const void* dY, int64_t T, int64_t lddy, const uint8_t* ckpt,
     const dim3 grid(static_cast<unsigned>(p.tiles), static_cast<unsigned>(p.strips));
     if (dtype == BIMASK_BF16)
         hipLaunchKernelGGL(k_act_bwd<uint16_t>, grid, dim3(kThreads), 0, s, static_cast<const uint16_t*>(dY), T, lddy, ckpt, scales, I, act,
-                           static_cast<uint16_t*>(dZ), lddz, sums, pitch, p.rows, per_row, p.log2c, whole_rows<uint16_t>(dY, lddy),
-                           whole_rows<uint16_t>(dZ, lddz));
+                           static_cast<uint16_t*>(dZ), lddz, sums, pitch, p.rows, per_row, p.log2c);
     else
         hipLaunchKernelGGL(k_act_bwd<uint32_t>, grid, dim3(kThreads), 0, s, static_cast<const uint32_t*>(dY), T, lddy, ckpt, scales, I, act,
-                           static_cast<uint32_t*>(dZ), lddz, sums, pitch, p.rows, per_row, p.log2c, whole_rows<uint32_t>(dY, lddy),
-                           whole_rows<uint32_t>(dZ, lddz));
+                           static_cast<uint32_t*>(dZ), lddz, sums, pitch, p.rows, per_row, p.log2c);
     if (int rc = check_launch()) return rc;
     if (dbias && p.strips > 1) {
-        hipLaunchKernelGGL(k_sum_strips, dim3(static_cast<unsigned>(ceil_div(I, kThreads))), dim3(kThreads), 0, s, ws, static_cast<int>(p.strips),
+        hipLaunchKernelGGL(k_sum_strips, dim3(static_cast<unsigned>(ceil_div(I, 16))), dim3(kThreads), 0, s, ws, static_cast<int>(p.strips),
                            pitch, I, dbias);
         return check_launch();
     }

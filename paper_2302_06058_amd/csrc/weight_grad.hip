@@ -1,12 +1,13 @@
 // Dense weight gradient of the straight-through estimator (arXiv 2302.06058, Sec. 3.1) from an 8-bit checkpoint of the layer's input:
 //     dW[i][j] = sum_t dY[t][i] * X~[t][j]
 //
-// Both operands lie with the contraction index t as their slow dimension.  A stage of 64 tokens goes to LDS as it lies in memory
+// Both operands lie with the contraction index t as their slow dimension.  A stage of 32 tokens goes to LDS as it lies in memory
 // (the codes put back to bf16 on the way: code * 2^e is exact in bf16), and the transposing LDS read hands every lane the
 // consecutive tokens of its row that the matrix instruction wants.  16 lanes of such a read touch four token rows at 32 bytes
 // each: the 64-byte chunks of a row are XOR-swizzled by the row so that they fall into different banks.
 // Few output tiles and many tokens: workgroups split the tokens, their fp32 sums go to the workspace and are added in order.
 #include "act.hpp"
+#include <type_traits>
 
 namespace bimask {
 namespace {
@@ -18,13 +19,14 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kStageT = 64;                              // tokens per stage
+constexpr int kStageT = 32;                              // tokens per stage
 
 union Frag { bf16x8 v; u32x2 d[2]; };
 
 // 4 consecutive tokens of one row per lane, 16 lanes: 4 tokens x 16 rows
-__device__ __forceinline__ u32x2 read_turned(const uint8_t* p) {
-    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p)));
+__device__ __forceinline__ u32x2 read_turned(uint32_t lds, int ofs) {
+    typedef __attribute__((address_space(3))) char lds_char;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)((lds_char*)lds + ofs)));
 }
 
 enum OutMode { kOutF32 = 0, kOutBF16 = 1, kAddF32 = 2, kAddBF16 = 3 };
@@ -48,78 +50,126 @@ __device__ __forceinline__ void put(int mode, void* out, int64_t at, float v) {
     else put<kAddBF16>(out, at, v);
 }
 
-// BM x BN output tile on WM x WN wavefronts.  WHOLE: rows of dY start on 16 bytes and I is a multiple of 8.
-// blockIdx.y: pieces of `rows` tokens; with more than one the sums go to part + blockIdx.y * I * J.
-template <int BM, int BN, int WM, int WN, bool WHOLE>
-__global__ void __launch_bounds__(64 * WM * WN)
+// BM x BN output tile on WM x WN wavefronts.  WHOLE: I >= 8 and 32 rows of either operand span less than 2^31 bytes.  Rows of dY
+// may start on any element (the 16-byte loads need no more).  Where I is no multiple of 8, the piece that would run over the row's
+// end is the row's last 8 features instead: its first `over` rows of the output come twice, the others `over` places late.
+// Pieces of `rows` tokens; with more than one the sums go to part + piece * I * J.
+//
+// Stages of 32 tokens pass through three LDS buffers: while stage s is multiplied, stage s + 2 (requested SETS stages ago, one register
+// set each) is put back to bf16 and written, stage s + 2 + SETS is requested, and the first fragments of stage s + 1, complete since the last barrier,
+// are read: a stage ends with one barrier and no wait for LDS or memory.  With WHOLE the loads are buffer loads of the piece's rows:
+// what lies beyond the last token reads as zero without a comparison, and an address is a scalar base and a constant per thread.
+// Columns beyond I or J are multiplied and not stored.
+template <int BM, int BN, int WM, int WN, int SETS, bool WHOLE>
+__global__ void __launch_bounds__(64 * WM * WN, 2)
 k_weight_grad(const uint16_t* __restrict__ dY, int64_t T, int64_t lddy, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
-              int64_t I, int64_t J, void* out, int64_t ldo, int mode, float* part, int tiles_j, int tiles, int64_t rows) {
+              int64_t I, int64_t J, void* out, int64_t ldo, int mode, float* part, uint32_t tiles_j, uint32_t tiles, uint32_t pieces, int64_t rows) {
     constexpr int NT = 64 * WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
-    constexpr int PA = kStageT * BM / 8 / NT, PB = kStageT * BN / 16 / NT;       // 16-byte pieces per thread and stage
+    constexpr int PA = kStageT * BM / 8 / NT, PB = (kStageT * BN / 16 + NT - 1) / NT;       // 16-byte pieces per thread and stage
     constexpr int SA = kStageT * BM * 2, SB = kStageT * BN * 2;                  // LDS bytes of a stage
-    static_assert(PA >= 1 && PB >= 1, "a piece for every thread");
+    static_assert(PA >= 1, "a piece for every thread");
     extern __shared__ u32x4 smem_u4[];
     uint8_t* smem = reinterpret_cast<uint8_t*>(smem_u4);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave % WM, wn = wave / WM, l32 = lane & 31, h = lane >> 5;
-    // XCD x takes a contiguous run of tiles, so that its L2 serves the token rows of neighbours
-    const int per_xcd = (tiles + 7) / 8, n = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-    if ((blockIdx.x >> 3) >= static_cast<unsigned>(per_xcd) || n >= tiles) return;
-    const int64_t i0 = static_cast<int64_t>(n / tiles_j) * BM, j0 = static_cast<int64_t>(n % tiles_j) * BN;
-    const int64_t t_begin = blockIdx.y * rows, t_end = t_begin + rows < T ? t_begin + rows : T;
+    // XCD x takes a contiguous run of (piece, tile) pairs, tiles fastest, so that its L2 serves the token rows of neighbours
+    const uint32_t total = static_cast<uint32_t>(tiles) * static_cast<uint32_t>(pieces), per_xcd = (total + 7) / 8;
+    const uint32_t n = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if (n >= total) return;
+    const uint32_t piece = n / tiles, tile = n - piece * tiles;
+    const int64_t i0 = static_cast<int64_t>(tile / tiles_j) * BM, j0 = static_cast<int64_t>(tile % tiles_j) * BN;
+    const int64_t t_begin = piece * rows, t_end = t_begin + rows < T ? t_begin + rows : T;
     const int64_t pitch = ckpt_pitch(J), blocks = ckpt_blocks(J);
+    const int stages = static_cast<int>(t_begin < t_end ? ceil_div(t_end - t_begin, kStageT) : 0);
+
+    const bool has_b = kStageT * BN / 16 >= NT || tid < kStageT * BN / 16;        // 64 columns: codes for half of the threads
 
     auto swz_a = [](int row) { return BM >= 128 ? row & 3 : (row >> 1) & 1; };
     auto swz_b = [](int row) { return BN >= 128 ? row & 3 : (row >> 1) & 1; };
 
-    u32x4 ra[PA], rb[PB];
-    int rs[PB];
-    auto load = [&](int64_t t0) {
+    u32x4 ra[SETS][PA], rb[SETS][PB];
+    int rs[SETS][PB];
+    uint32_t off_a[PA], off_b[PB], off_s[PB];
+    if constexpr (WHOLE) {
 #pragma unroll
         for (int p = 0; p < PA; ++p) {
             const int q = tid + NT * p, row = q / (BM / 8), u = q % (BM / 8);
-            const int64_t t = t0 + row, i = i0 + 8 * u;
-            if constexpr (WHOLE) {
-                const bool in = t < t_end && i < I;
-                const u32x4 v = *reinterpret_cast<const u32x4*>(dY + (in ? t * lddy + i : 0));
-                ra[p] = in ? v : (u32x4){0u, 0u, 0u, 0u};
-            } else {
-                ra[p] = (u32x4){0u, 0u, 0u, 0u};
+            off_a[p] = static_cast<uint32_t>((row * lddy + (i0 + 8 * u + 8 <= I ? i0 + 8 * u : I - 8)) * 2);
+        }
+#pragma unroll
+        for (int p = 0; p < PB; ++p) {
+            const int q = tid + NT * p, row = q / (BN / 16), u = q % (BN / 16);
+            const int64_t j = j0 + 16 * u < pitch && has_b ? j0 + 16 * u : 0;
+            off_b[p] = static_cast<uint32_t>((has_b ? row : 0) * pitch + j);
+            off_s[p] = static_cast<uint32_t>((has_b ? row : 0) * blocks + j / 32);
+        }
+    }
+    // WHOLE: the rows of the next stage to request, as buffers that end with the piece's last row
+    const uint16_t* next_a = dY + t_begin * lddy;
+    const uint8_t *next_b = codes + t_begin * pitch, *next_s = scales + t_begin * blocks;
+    int rows_left = static_cast<int>(t_end - t_begin);
+    const int row_a = static_cast<int>(lddy * 2), last_a = static_cast<int>(I * 2), row_b = static_cast<int>(pitch), row_s = static_cast<int>(blocks);
+    auto load = [&](int set, int st) {
+        if constexpr (WHOLE) {
+            const int n = rows_left < kStageT ? rows_left : kStageT, some = n > 0 ? -1 : 0;
+            const auto A = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(next_a), 0, ((n - 1) * row_a + last_a) & some, 0x00020000);
+            const auto B = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(next_b), 0, (n * row_b) & some, 0x00020000);
+            const auto S = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(next_s), 0, (n * row_s) & some, 0x00020000);
+            next_a += kStageT * lddy;                    // (past the end they are not read through: their buffers are empty)
+            next_b += kStageT * pitch;
+            next_s += kStageT * blocks;
+            rows_left -= kStageT;
+#pragma unroll
+            for (int p = 0; p < PA; ++p) ra[set][p] = __builtin_amdgcn_raw_buffer_load_b128(A, off_a[p], 0, 0);
+#pragma unroll
+            for (int p = 0; p < PB; ++p) {
+                rb[set][p] = __builtin_amdgcn_raw_buffer_load_b128(B, off_b[p], 0, 0);
+                rs[set][p] = __builtin_amdgcn_raw_buffer_load_b8(S, off_s[p], 0, 0);
+            }
+        } else {
+            const int64_t t0 = t_begin + static_cast<int64_t>(st) * kStageT;
+#pragma unroll
+            for (int p = 0; p < PA; ++p) {
+                const int q = tid + NT * p, row = q / (BM / 8), u = q % (BM / 8);
+                const int64_t t = t0 + row, i = i0 + 8 * u;
+                ra[set][p] = (u32x4){0u, 0u, 0u, 0u};
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (t < t_end && i + e < I) ra[p][e >> 1] |= static_cast<uint32_t>(dY[t * lddy + i + e]) << (16 * (e & 1));
+                    if (t < t_end && i + e < I) ra[set][p][e >> 1] |= static_cast<uint32_t>(dY[t * lddy + i + e]) << (16 * (e & 1));
+            }
+#pragma unroll
+            for (int p = 0; p < PB; ++p) {
+                const int q = tid + NT * p, row = q / (BN / 16), u = q % (BN / 16);
+                const int64_t t = t0 + row, j = j0 + 16 * u;
+                const bool in = has_b && t < t_end && j < pitch;
+                const u32x4 v = *reinterpret_cast<const u32x4*>(codes + (in ? t * pitch + j : 0));
+                rb[set][p] = in ? v : (u32x4){0u, 0u, 0u, 0u};
+                rs[set][p] = in ? scales[t * blocks + j / 32] : 0;
             }
         }
-#pragma unroll
-        for (int p = 0; p < PB; ++p) {
-            const int q = tid + NT * p, row = q / (BN / 16), u = q % (BN / 16);
-            const int64_t t = t0 + row, j = j0 + 16 * u;
-            const bool in = t < t_end && j < pitch;
-            const u32x4 v = *reinterpret_cast<const u32x4*>(codes + (in ? t * pitch + j : 0));
-            rb[p] = in ? v : (u32x4){0u, 0u, 0u, 0u};
-            rs[p] = in ? scales[t * blocks + j / 32] : 0;
-        }
     };
-    auto stage = [&](uint8_t* s) {
+    auto stage_a = [&](int set, uint8_t* s) {
 #pragma unroll
         for (int p = 0; p < PA; ++p) {
             const int q = tid + NT * p, row = q / (BM / 8), u = q % (BM / 8);
-            *reinterpret_cast<u32x4*>(s + row * (BM * 2) + (((u >> 2) ^ swz_a(row)) << 6) + ((u & 3) << 4)) = ra[p];
+            *reinterpret_cast<u32x4*>(s + row * (BM * 2) + (((u >> 2) ^ swz_a(row)) << 6) + ((u & 3) << 4)) = ra[set][p];
         }
+    };
+    auto stage_b = [&](int set, uint8_t* s, int first, int end) {
 #pragma unroll
-        for (int p = 0; p < PB; ++p) {
+        for (int p = first; p < end; ++p) {
             const int q = tid + NT * p, row = q / (BN / 16), u = q % (BN / 16);
-            const float scale = ckpt_scale(rs[p]);
+            const float scale = ckpt_scale(rs[set][p]);
             uint8_t* dst = s + SA + row * (BN * 2) + (((u >> 1) ^ swz_b(row)) << 6) + ((u & 1) << 5);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 u32x4 v;
 #pragma unroll
                 for (int d = 0; d < 4; ++d) {
-                    const uint32_t four = rb[p][2 * x + (d >> 1)];
+                    const uint32_t four = rb[set][p][2 * x + (d >> 1)];
                     v[d] = pack_bf16(ckpt_value(four, 2 * (d & 1), scale), ckpt_value(four, 2 * (d & 1) + 1, scale));
                 }
-                *reinterpret_cast<u32x4*>(dst + 16 * x) = v;
+                if (has_b) *reinterpret_cast<u32x4*>(dst + 16 * x) = v;
             }
         }
     };
@@ -140,51 +190,109 @@ k_weight_grad(const uint16_t* __restrict__ dY, int64_t T, int64_t lddy, const ui
 #pragma unroll
     for (int j = 0; j < TN; ++j) fb[j] = SA + krow * (BN * 2) + (((wn * TN + j) ^ swz_b(krow)) << 6) + in_chunk;
 
-    const int64_t stages = t_begin < t_end ? ceil_div(t_end - t_begin, kStageT) : 0;
-    if (stages > 0) {
-        load(t_begin);
-        stage(smem);
-    }
-    __syncthreads();
-    for (int64_t st = 0; st < stages; ++st) {
-        uint8_t* cur = smem + (st & 1) * (SA + SB);
-        const bool more = st + 1 < stages;
-        if (more) load(t_begin + (st + 1) * kStageT);
+    Frag a[2][TM], b[2][TN];
+    auto read = [&](int slot, uint32_t buf, int ks) {
 #pragma unroll
-        for (int ks = 0; ks < kStageT / 16; ++ks) {
-            Frag a[TM], b[TN];
+        for (int x = 0; x < 2; ++x) {
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
+            for (int i = 0; i < TM; ++i) a[slot][i].d[x] = read_turned(buf + fa[i], (16 * ks + 4 * x) * (BM * 2));
 #pragma unroll
-                for (int i = 0; i < TM; ++i) a[i].d[x] = read_turned(cur + fa[i] + (16 * ks + 4 * x) * (BM * 2));
-#pragma unroll
-                for (int j = 0; j < TN; ++j) b[j].d[x] = read_turned(cur + fb[j] + (16 * ks + 4 * x) * (BN * 2));
-            }
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i].v, b[j].v, acc[i][j], 0, 0, 0);
+            for (int j = 0; j < TN; ++j) b[slot][j].d[x] = read_turned(buf + fb[j], (16 * ks + 4 * x) * (BN * 2));
         }
-        if (more) stage(smem + ((st + 1) & 1) * (SA + SB));
+    };
+    auto multiply = [&](int slot) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[slot][i].v, b[slot][j].v, acc[i][j], 0, 0, 0);
+    };
+    // the order in which the compiler is to mix the instructions of a half stage: reads and the rest between matrix instructions
+    auto mix = [&]() {
+#pragma unroll
+        for (int k = 0; k < TM * TN; ++k) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                                          // matrix
+            __builtin_amdgcn_sched_group_barrier(0x100, (2 * (TM + TN) + TM * TN - 1) / (TM * TN), 0);  // LDS read
+            __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);                                          // ALU
+            __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);                                          // LDS write
+            __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);                                          // memory read
+        }
+    };
+
+    if (stages > 0) {
+        load(0, 0);
+        load(1, 1);
+        stage_a(0, smem);
+        stage_b(0, smem, 0, PB);
+        load(0, 2);
+        stage_a(1, smem + (SA + SB));
+        stage_b(1, smem + (SA + SB), 0, PB);
+#pragma unroll
+        for (int k = 1; k < SETS; ++k) load(k, k + 2);
         __syncthreads();
+        const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)smem));
+        uint32_t cur = 0, next = SA + SB, after = 2 * (SA + SB);
+        read(0, lds + cur, 0);
+        auto step = [&](auto set_c, int st) {
+            constexpr int set = decltype(set_c)::value;
+            read(1, lds + cur, 1);
+            multiply(0);
+            stage_a(set, smem + after);
+            stage_b(set, smem + after, 0, PB > 1 ? PB / 2 : 0);
+            mix();
+            __builtin_amdgcn_sched_barrier(0);
+            read(0, lds + next, 0);
+            multiply(1);
+            stage_b(set, smem + after, PB > 1 ? PB / 2 : 0, PB);
+            load(set, st + 2 + SETS);
+            mix();
+            __builtin_amdgcn_sched_barrier(0);
+            __syncthreads();
+            const uint32_t x = cur;
+            cur = next;
+            next = after;
+            after = x;
+        };
+#pragma unroll 1
+        for (int st = 0; st < stages; st += SETS) {      // (a stage beyond the last is one of zeros)
+            step(std::integral_constant<int, 0>{}, st);
+            step(std::integral_constant<int, 1>{}, st + 1);
+            if constexpr (SETS == 4) {
+                step(std::integral_constant<int, 2>{}, st + 2);
+                step(std::integral_constant<int, 3>{}, st + 3);
+            }
+        }
     }
 
-    const bool split = gridDim.y > 1;
-    void* dst = split ? static_cast<void*>(part + static_cast<int64_t>(blockIdx.y) * I * J) : out;
+    // Output: 32 rows of a wavefront at a time through an LDS strip of its own, so that rows leave as segments of 32 TN columns.
+    const bool split = pieces > 1;
+    void* dst = split ? static_cast<void*>(part + static_cast<int64_t>(piece) * I * J) : out;
     const int64_t ld = split ? J : ldo;
-    const int m = split ? kOutF32 : mode;
+    constexpr int COLS = 32 * TN, PITCH = COLS + 4;
+    static_assert(WM * WN * 32 * PITCH * 4 <= 3 * (SA + SB) && COLS % 64 == 0, "strips fit the stage buffers");
+    float* strip = reinterpret_cast<float*>(smem) + wave * (32 * PITCH);
+    const int64_t col0 = j0 + wn * COLS + lane;
+    __syncthreads();                                     // every wavefront is done with the stage buffers
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+    for (int i = 0; i < TM; ++i) {
+        const int64_t row0 = i0 + (wm * TM + i) * 32;
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const int64_t col = j0 + (wn * TN + j) * 32 + l32;
-            if (col < J)
+        for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int q = 0; q < 16; ++q) {
-                    const int64_t row = i0 + (wm * TM + i) * 32 + 8 * (q >> 2) + 4 * h + (q & 3);
-                    if (row < I) put(m, dst, row * ld + col, acc[i][j][q]);
-                }
-        }
+            for (int q = 0; q < 16; ++q) strip[(8 * (q >> 2) + 4 * h + (q & 3)) * PITCH + 32 * j + l32] = acc[i][j][q];
+        const int over = WHOLE ? static_cast<int>(-I & 7) : 0, n_rows = static_cast<int>(I - row0 < 32 ? I - row0 : 32);
+        const int late = I - row0 < 32 ? n_rows & ~7 : 32;              // from this row on
+        auto write = [&](auto mode_c) {
+#pragma unroll 4
+            for (int r = 0; r < n_rows; ++r)
+#pragma unroll
+                for (int c = 0; c < COLS; c += 64)
+                    if (col0 + c < J) put<decltype(mode_c)::value>(dst, (row0 + r) * ld + col0 + c, strip[(r + (r >= late ? over : 0)) * PITCH + c + lane]);
+        };
+        if (split || mode == kOutF32) write(std::integral_constant<int, kOutF32>{});
+        else if (mode == kOutBF16) write(std::integral_constant<int, kOutBF16>{});
+        else if (mode == kAddF32) write(std::integral_constant<int, kAddF32>{});
+        else write(std::integral_constant<int, kAddBF16>{});
+    }
 }
 
 // fp32: 64 x 64 tiles on four wavefronts, fp32 matrix instructions, whose operands are one element per lane: LDS rows as they lie.
@@ -254,14 +362,26 @@ k_weight_grad_f32(const float* __restrict__ dY, int64_t T, int64_t lddy, const u
         }
 }
 
+// 64 elements x 4 ranges of pieces per workgroup, added in a fixed order on both levels
 __global__ void __launch_bounds__(kThreads)
 k_sum_pieces(const float* __restrict__ part, int pieces, int64_t I, int64_t J, void* out, int64_t ldo, int mode) {
+    __shared__ float sums[4][64];
+    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
     const int64_t total = I * J;
-    for (int64_t e = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; e < total; e += static_cast<int64_t>(gridDim.x) * kThreads) {
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * 64; first < total; first += static_cast<int64_t>(gridDim.x) * 64) {
+        const int64_t e = first + x;
         float s = 0.f;
-        for (int k = 0; k < pieces; ++k) s += part[k * total + e];
-        const int64_t i = e / J;
-        put(mode, out, i * ldo + (e - i * J), s);
+        if (e < total) {
+#pragma unroll 8
+            for (int k = y; k < pieces; k += 4) s += part[k * total + e];
+        }
+        sums[y][x] = s;
+        __syncthreads();
+        if (y == 0 && e < total) {
+            const int64_t i = e / J;
+            put(mode, out, i * ldo + (e - i * J), ((sums[0][x] + sums[1][x]) + sums[2][x]) + sums[3][x]);
+        }
+        __syncthreads();
     }
 }
 
@@ -270,10 +390,10 @@ struct Operands {
     hipStream_t s;
 };
 
-template <int BM, int BN, int WM, int WN, bool WHOLE>
-int run_t(const Operands& o, const WeightGradPlan& p) {
-    constexpr int lds = 2 * kStageT * (BM + BN) * 2;
-    auto kern = k_weight_grad<BM, BN, WM, WN, WHOLE>;
+template <int BM, int BN, int WM, int WN, int SETS, bool WHOLE>
+int run(const Operands& o, const WeightGradPlan& p) {
+    constexpr int lds = 3 * kStageT * (BM + BN) * 2;
+    auto kern = k_weight_grad<BM, BN, WM, WN, SETS, WHOLE>;
     if (lds > 48 * 1024) {
         static DeviceMemo attr_set;
         const int dev = DeviceMemo::device();
@@ -283,18 +403,12 @@ int run_t(const Operands& o, const WeightGradPlan& p) {
             attr_set.set(dev, 1);
         }
     }
-    const int64_t tiles = ceil_div(o.I, BM) * ceil_div(o.J, BN), grid = round_up(tiles, 8);
+    const int64_t tiles = ceil_div(o.I, BM) * ceil_div(o.J, BN), grid = round_up(tiles * p.pieces, 8);
     if (grid * (64 * WM * WN) > 0xFFFFFFFFll) return BIMASK_ERR_SHAPE;
-    hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(grid), static_cast<unsigned>(p.pieces)), dim3(64 * WM * WN), lds, o.s,
+    hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(grid)), dim3(64 * WM * WN), lds, o.s,
                        static_cast<const uint16_t*>(o.dY), o.T, o.lddy, o.codes, o.scales, o.I, o.J, o.dW, o.lddw, o.mode, o.part,
-                       static_cast<int>(ceil_div(o.J, BN)), static_cast<int>(tiles), p.rows);
+                       static_cast<uint32_t>(ceil_div(o.J, BN)), static_cast<uint32_t>(tiles), static_cast<uint32_t>(p.pieces), p.rows);
     return check_launch();
-}
-
-template <int BM, int BN, int WM, int WN>
-int run(const Operands& o, const WeightGradPlan& p) {
-    const bool whole = aligned16(o.dY) && o.lddy % 8 == 0 && o.I % 8 == 0;
-    return whole ? run_t<BM, BN, WM, WN, true>(o, p) : run_t<BM, BN, WM, WN, false>(o, p);
 }
 
 }  // namespace
@@ -302,11 +416,14 @@ int run(const Operands& o, const WeightGradPlan& p) {
 WeightGradPlan plan_weight_grad(int64_t T, int64_t I, int64_t J, int dtype) {
     WeightGradPlan p;
     const bool f32 = dtype == BIMASK_F32;
-    p.big = !f32 && ceil_div(I, 256) * ceil_div(J, 256) >= 192;
-    const int64_t bm = f32 ? kTileF32 : p.big ? 256 : 128, stage = f32 ? kStageF32 : kStageT;
-    const int64_t tiles = ceil_div(I, bm) * ceil_div(J, bm), stages = ceil_div(T, stage);
-    // pieces: about 512 workgroups, none with fewer than 8 stages
-    int64_t pieces = p.big || tiles >= 512 ? 1 : ceil_div(512, tiles);
+    p.tile = ceil_div(I, 256) * ceil_div(J, 256) >= 192 ? WeightGradPlan::k256x256
+           : I <= 64 && J > 64 ? WeightGradPlan::k64x256 : J <= 64 && I > 64 ? WeightGradPlan::k256x64 : WeightGradPlan::k128x128;
+    const bool big = !f32 && p.tile == WeightGradPlan::k256x256;
+    const int64_t bm = f32 ? kTileF32 : p.tile == WeightGradPlan::k64x256 ? 64 : p.tile == WeightGradPlan::k256x64 ? 256 : 128;
+    const int64_t bn = f32 ? kTileF32 : p.tile == WeightGradPlan::k64x256 ? 256 : p.tile == WeightGradPlan::k256x64 ? 64 : 128;
+    const int64_t tiles = ceil_div(I, bm) * ceil_div(J, bn), stage = f32 ? kStageF32 : kStageT, stages = ceil_div(T, stage);
+    // pieces: at most 512 workgroups (two per CU are there at once; a few more would run after them), none with fewer than 8 stages
+    int64_t pieces = big || tiles > 256 ? 1 : 512 / tiles;
     const int64_t most = stages / 8 > 1 ? stages / 8 : 1;
     pieces = pieces < most ? pieces : most;
     p.rows = ceil_div(stages, pieces) * stage;
@@ -329,11 +446,15 @@ int launch_weight_grad(const void* dY, int64_t T, int64_t lddy, const uint8_t* c
                            static_cast<int>(tiles), p.rows);
         rc = check_launch();
     } else {
-        rc = p.big ? run<256, 256, 2, 4>(o, p) : run<128, 128, 2, 2>(o, p);
+        if (I < 8 || lddy >= (1 << 24) || J >= (1 << 25) || T >= (1ll << 31)) rc = run<128, 128, 2, 2, 2, false>(o, p);
+        else if (p.tile == WeightGradPlan::k256x256) rc = run<256, 256, 2, 4, 2, true>(o, p);
+        else if (p.tile == WeightGradPlan::k64x256) rc = run<64, 256, 1, 4, 4, true>(o, p);
+        else if (p.tile == WeightGradPlan::k256x64) rc = run<256, 64, 4, 1, 4, true>(o, p);
+        else rc = run<128, 128, 2, 2, 4, true>(o, p);
     }
     if (rc || p.pieces == 1) return rc;
-    const int64_t n = ceil_div(I * J, kThreads);
-    hipLaunchKernelGGL(k_sum_pieces, dim3(static_cast<unsigned>(n < 4096 ? n : 4096)), dim3(kThreads), 0, s, ws, static_cast<int>(p.pieces), I, J,
+    const int64_t n = ceil_div(I * J, 64);
+    hipLaunchKernelGGL(k_sum_pieces, dim3(static_cast<unsigned>(n < (1 << 20) ? n : 1 << 20)), dim3(kThreads), 0, s, ws, static_cast<int>(p.pieces), I, J,
                        dW, lddw, mode);
     return check_launch();
 }
