@@ -11,7 +11,10 @@ namespace bimask {
 // exactly 0 at both ends, where the other factors are finite.  gelu is z * Phi(z) with Phi's tail 0.5 erfc(|z| / sqrt 2) =
 // exp(-z^2 / 2) R(|z|); R (the Mills ratio over sqrt(2 pi)) as t * polynomial(t), t = 1 / (1 + 0.3 |z|): least squares on the
 // relative error, re-weighted to equal peaks, 1.5e-7 over 0 <= |z| <= 14.  The tail itself never comes from 1 - Phi.
-// Cost of a value in issue slots (2^x and 1/x take four each): silu 11, gelu_tanh 13, gelu 24; slopes 12, 17, 25.
+// COARSE, for results that are rounded to bf16 (2^-9): gelu as max(z, 0) - |z| Q(|z|), log2 Q a polynomial fitted over 0 .. 5.5 (Q off
+// by 2.5e-4 = 2^-12 of itself there; beyond, where Q < 2e-8, it keeps falling).  Slopes have no such form: the bias gradient that sums
+// them is fp32.
+// Cost of a value in issue slots (2^x and 1/x take four each): silu 11, gelu_tanh 13, gelu 24, coarse 12; slopes 12, 17, 25.
 constexpr float kLog2e = 1.44269504f, kTanhC1 = 1.5957691216f, kTanhC2 = 0.0713548163f;       // 2 sqrt(2/pi), times 0.044715
 
 __device__ __forceinline__ float sigma_of(float minus_u_log2e) {
@@ -34,7 +37,7 @@ __device__ __forceinline__ float phi_cdf(float z, float g) {
 }
 
 // z -> act(z), for n values; act is uniform
-template <int n>
+template <bool COARSE, int n>
 __device__ __forceinline__ void apply_act(float (&z)[n], int act) {
     if (act == BIMASK_ACT_NONE) return;
     if (act == BIMASK_ACT_RELU) {
@@ -42,7 +45,20 @@ __device__ __forceinline__ void apply_act(float (&z)[n], int act) {
         for (int i = 0; i < n; ++i) z[i] = z[i] <= 0.f ? 0.f : z[i];         // (NaN stays)
     } else if (act == BIMASK_ACT_GELU) {
 #pragma unroll
-        for (int i = 0; i < n; ++i) z[i] *= phi_cdf(z[i], gauss(z[i]));
+        for (int i = 0; i < n; ++i) {
+            if constexpr (COARSE) {
+                const float a = __builtin_fabsf(z[i]);
+                float p = __builtin_fmaf(-2.33251254e-4f, a, 4.86977249e-3f);
+                p = __builtin_fmaf(p, a, -4.45990033e-2f);
+                p = __builtin_fmaf(p, a, -0.469681115f);
+                p = __builtin_fmaf(p, a, -1.14626077f);
+                p = __builtin_fmaf(p, a, -1.0003591f);
+                // (Q of an infinity is 0 and of a NaN NaN; the factor beside it is finite, so that an infinity stays one)
+                z[i] = __builtin_fmaf(-__builtin_fminf(a, 3.4e38f), __builtin_amdgcn_exp2f(p), __builtin_fmaxf(z[i], 0.f));
+            } else {
+                z[i] *= phi_cdf(z[i], gauss(z[i]));
+            }
+        }
     } else if (act == BIMASK_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < n; ++i) z[i] *= sigma_of(-kLog2e * z[i]);
@@ -104,15 +120,25 @@ __device__ __forceinline__ float ckpt_inverse(int byte) { return __builtin_bit_c
 __device__ __forceinline__ float ckpt_scale(int byte) {
     return __builtin_bit_cast(float, byte == kCkptNaN ? 0x7FC00000u : static_cast<uint32_t>(byte) << 23);
 }
-// 4 values -> 4 codes, first in the low byte; `inv` 0 for a block that reads as NaN (its codes are written as 0)
-__device__ __forceinline__ uint32_t ckpt_codes(const float* v, float inv, bool bad) {
-    uint32_t r = 0;
+// n values of a block -> their codes, four a word, first in the low byte.  v * 2^-e is exact, so adding 1.5 * 2^23 rounds it to an
+// integer (halves to even) whose two's complement stands in the low byte of the sum.
+template <int n>
+__device__ __forceinline__ void ckpt_encode(float (&v)[n], int byte, uint32_t (&out)[n / 4]) {
+    const bool bad = byte == kCkptNaN;
+    const float inv = ckpt_inverse(bad ? 127 : byte);
+    if (byte == 248) {                                   // e is kept to 121: up to 128 steps
+        const float most = 127.f * ckpt_scale(248);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float q = __builtin_fminf(__builtin_fmaxf(__builtin_rintf(v[i] * inv), -127.f), 127.f);
-        r |= (static_cast<uint32_t>(static_cast<int>(q)) & 0xFFu) << (8 * i);
+        for (int i = 0; i < n; ++i) v[i] = __builtin_fminf(__builtin_fmaxf(v[i], -most), most);
     }
-    return bad ? 0u : r;
+#pragma unroll
+    for (int w = 0; w < n / 4; ++w) {
+        uint32_t q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = __builtin_bit_cast(uint32_t, __builtin_fmaf(v[4 * w + i], inv, 12582912.f));
+        const uint32_t lo = __builtin_amdgcn_perm(q[1], q[0], 0x0C0C0400u), hi = __builtin_amdgcn_perm(q[3], q[2], 0x0C0C0400u);
+        out[w] = bad ? 0u : lo | hi << 16;
+    }
 }
 __device__ __forceinline__ float ckpt_value(uint32_t four, int i, float scale) {      // code i of 4
     return static_cast<float>(static_cast<int8_t>(four >> (8 * i))) * scale;

@@ -123,10 +123,9 @@ k_checkpoint_store(const raw* __restrict__ X, int64_t T, int64_t J, int64_t ldx,
         }
         const uint32_t other = __shfl_xor(most, 1);
         const int byte = ckpt_scale_byte(other > most ? other : most);
-        const float inv = ckpt_inverse(byte == kCkptNaN ? 127 : byte);
-        u32x4 out;
-#pragma unroll
-        for (int d = 0; d < 4; ++d) out[d] = ckpt_codes(f + 4 * d, inv, byte == kCkptNaN);
+        uint32_t four[4];
+        ckpt_encode(f, byte, four);
+        const u32x4 out = {four[0], four[1], four[2], four[3]};
         *reinterpret_cast<u32x4*>(codes + (p.t * per_row + p.half) * kPiece) = out;
         if (!(p.half & 1)) scales[p.t * (per_row / 2) + p.half / 2] = static_cast<uint8_t>(byte);
     }

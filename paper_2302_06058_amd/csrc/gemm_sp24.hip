@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(64 * WAVES_M * WAVES_N * KG)
 k_gemm_sp24(const uint16_t* __restrict__ A, const uint32_t* __restrict__ Ameta, int64_t Adim, int64_t K,
             const uint16_t* __restrict__ Bm, int64_t T, int64_t ldb, uint16_t* __restrict__ C, int64_t ldc,
             int tiles_a, bool vecC) {
-    gemm_sp24_body<BM, BN, WAVES_M, WAVES_N, KG, PF, BGUARD, BHALF, KTAIL, DENSE>(A, Ameta, Adim, K, Bm, T, ldb, C, ldc, tiles_a, vecC, PlainOut{});
+    gemm_sp24_body<BM, BN, WAVES_M, WAVES_N, KG, PF, BGUARD, BHALF, KTAIL, DENSE, BN>(A, Ameta, Adim, K, Bm, T, ldb, C, ldc, tiles_a, vecC, PlainOut{});
 }
 
 template <int BM, int BN, int WAVES_M, int WAVES_N, int KG, int PF, bool BGUARD, bool BHALF, bool KTAIL = false, bool DENSE = false>

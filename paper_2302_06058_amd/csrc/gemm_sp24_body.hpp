@@ -60,7 +60,8 @@ __device__ __forceinline__ u32x4 load_guarded(const uint16_t* row, int64_t k, in
 // 23.1 -> 12.7).  Where the tiles fill the chip it gains nothing: the bytes every CU pulls through its L1 set the pace
 // there, not the wavefronts in flight (512 x 4608 at 3136 tokens, 128 x 64 tiles: 24.2 us with one group, 24.2 with two).
 // OUT: what becomes of the sums (PlainOut: rounded and written).
-template <int BM, int BN, int WAVES_M, int WAVES_N, int KG, int PF, bool BGUARD, bool BHALF, bool KTAIL, bool DENSE, class OUT>
+// TR: token rows that are fetched (at most that many exist); what a fragment holds beyond them is multiplied and never stored.
+template <int BM, int BN, int WAVES_M, int WAVES_N, int KG, int PF, bool BGUARD, bool BHALF, bool KTAIL, bool DENSE, int TR, class OUT>
 __device__ __forceinline__ void
 gemm_sp24_body(const uint16_t* A, const uint32_t* Ameta, int64_t Adim, int64_t K,
                const uint16_t* Bm, int64_t T, int64_t ldb, uint16_t* C, int64_t ldc,
@@ -71,8 +72,8 @@ gemm_sp24_body(const uint16_t* A, const uint32_t* Ameta, int64_t Adim, int64_t K
     constexpr int TM = WM / 32, TN = WN / 32;
     constexpr int NBUF = PF + 1;
     constexpr int NTB = BHALF ? NT / 2 : NT;            // threads that fetch the token tile
-    constexpr int NB_ = BN * 16 / NTB;                  // 16-byte granules of Bm per fetching thread per stage
-    static_assert(NB_ >= 1 && (BN * 16) % NTB == 0, "token tile too small");
+    constexpr int NB_ = TR * 16 / NTB;                  // 16-byte granules of Bm per fetching thread per stage
+    static_assert(NB_ >= 1 && (TR * 16) % NTB == 0, "token tile too small");
     extern __shared__ u32x4 smem_u4[];
     uint8_t* smem = reinterpret_cast<uint8_t*>(smem_u4);
 
@@ -251,6 +252,11 @@ gemm_sp24_body(const uint16_t* A, const uint32_t* Ameta, int64_t Adim, int64_t K
     // straight to memory and neither evict the operands from L2 nor wait there as dirty lines.
     static_assert(BN * BM * 2 <= S::kTotal && (KG - 1) * BN * BM * 4 <= S::kTotal, "output tile must fit the stage buffers");
     __syncthreads();                                     // every wavefront is done with the last stage
+    if constexpr (OUT::kFused) {
+        constexpr int PASSES = (4 * KG * BN * BM + S::kTotal - 1) / S::kTotal;
+        out.template finish<BM, BN, WM, WN, TM, TN, NT * KG, KG, PASSES>(acc, smem, kg, wm, wn, lane, a0, t0, Adim, T, C, ldc, vecC);
+        return;
+    }
     if constexpr (KG > 1) {
         f32x4* part = reinterpret_cast<f32x4*>(smem_u4) + lane;      // [group - 1][wave][i][j][quad][lane]
         if (kg > 0) {
@@ -279,10 +285,6 @@ gemm_sp24_body(const uint16_t* A, const uint32_t* Ameta, int64_t Adim, int64_t K
                         }
         }
         __syncthreads();
-    }
-    if constexpr (OUT::kFused) {
-        out.template finish<BM, BN, WM, WN, TM, TN, NT * KG>(acc, smem, kg == 0, wm, wn, lane, a0, t0, Adim, T, C, ldc, vecC);
-        return;
     }
     if (kg == 0)
 #pragma unroll

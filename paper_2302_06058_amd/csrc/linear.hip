@@ -1,105 +1,34 @@
 // The linear layer's product with its epilogue:  Z = X (B .* W)^T + bias,  Y = act(Z) + residual  (operand of Eq. (3),
 // arXiv 2302.06058), on request with Z's 8-bit checkpoint.  linear_epilogue.hpp holds the epilogue; the main loops are those of
-// the plain products (gemm_sp24_body.hpp, gemm_f32_body.hpp) and, for few tokens, the kernel below.
+// the plain products (gemm_sp24_body.hpp, gemm_sp24_big_body.hpp, gemm_sp24_wide_body.hpp, gemm_f32_body.hpp).
 #include "gemm_sp24_body.hpp"
+#include "gemm_sp24_big_body.hpp"
+#include "gemm_sp24_wide_body.hpp"
 #include "gemm_f32_body.hpp"
 #include "linear_epilogue.hpp"
 
 namespace bimask {
 namespace {
 
-template <int BM, int BN, int WAVES_M, int WAVES_N, int KG, int PF, bool BGUARD, bool BHALF, bool KTAIL, bool DENSE>
+template <int BM, int BN, int WAVES_M, int WAVES_N, int KG, int PF, bool BGUARD, bool BHALF, bool KTAIL, bool DENSE, int TR>
 __global__ void __launch_bounds__(64 * WAVES_M * WAVES_N * KG)
 k_linear_sp24(const uint16_t* __restrict__ A, const uint32_t* __restrict__ Ameta, int64_t Adim, int64_t K,
               const uint16_t* __restrict__ Bm, int64_t T, int64_t ldb, uint16_t* C, int64_t ldc,
               int tiles_a, bool vecC, LinearOut out) {
-    gemm_sp24_body<BM, BN, WAVES_M, WAVES_N, KG, PF, BGUARD, BHALF, KTAIL, DENSE>(A, Ameta, Adim, K, Bm, T, ldb, C, ldc, tiles_a, vecC, out);
+    gemm_sp24_body<BM, BN, WAVES_M, WAVES_N, KG, PF, BGUARD, BHALF, KTAIL, DENSE, TR>(A, Ameta, Adim, K, Bm, T, ldb, C, ldc, tiles_a, vecC, out);
 }
 
-// Few tokens (single-token serving and small batches): the weights are read once and nothing else counts, so every workgroup
-// takes ONE row tile of 32 against up to 32 tokens and its wavefronts split the contraction, stage by stage, with two stages of
-// weight fragments (8.5 KB a wavefront) in flight each.  Token fragments come straight from the rows (L1 and L2 hold them).
-// The wavefronts' sums meet in LDS in wavefront order.
-constexpr int kFewWaves = 8;
+__global__ void __launch_bounds__(kBigThreads)
+k_linear_sp24_big(const uint16_t* __restrict__ A, const uint32_t* __restrict__ Ameta, int64_t Adim, int nk, const uint16_t* __restrict__ Bm,
+                  int64_t T, int64_t ldb, uint16_t* C, int64_t ldc, int tiles_a, int tiles_t, int tpx, LinearOut out) {
+    gemm_sp24_big_body(A, Ameta, Adim, nk, Bm, T, ldb, C, ldc, tiles_a, tiles_t, tpx, out);
+}
 
-template <bool GUARD, bool DENSE>
-__global__ void __launch_bounds__(64 * kFewWaves)
-k_linear_few(const uint16_t* __restrict__ A, const uint32_t* __restrict__ Ameta, int64_t Adim, int64_t K, const uint16_t* __restrict__ Bm,
-             int64_t T, int64_t ldb, uint16_t* C, int64_t ldc, bool vecC, LinearOut out) {
-    constexpr int NW = kFewWaves, NA = DENSE ? 8 : 4, U = DENSE ? 1 : 2;         // stages in flight
-    __shared__ f32x4 part[(NW - 1) * 4 * 64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int l32 = lane & 31, h = lane >> 5;
-    const int64_t rt = blockIdx.x, t0 = static_cast<int64_t>(blockIdx.y) * 32;
-    const int nk = static_cast<int>(ceil_div(K, SK));
-    const uint16_t* row = Bm + (t0 + l32 < T ? t0 + l32 : T - 1) * ldb;          // clamped: computed, never stored
-    const uint16_t* pa = A + (rt * nk * (NA * 64) + lane) * 8;
-    const uint32_t* pm = DENSE ? nullptr : Ameta + (rt * nk * 64 + lane) * 2;
-    f32x16 acc[1][1];
-#pragma unroll
-    for (int q = 0; q < 16; ++q) acc[0][0][q] = 0.f;
-    for (int st = wave; st < nk; st += NW * U) {
-        u32x4 ra[U][NA];
-        u32x2 rm[U];
-        BFrag b[U][4];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int kt = st + u * NW < nk ? st + u * NW : nk - 1;              // clamped: loaded, not used
-#pragma unroll
-            for (int g = 0; g < NA; ++g) ra[u][g] = *reinterpret_cast<const u32x4*>(pa + (static_cast<int64_t>(kt) * NA + g) * 512);
-            if constexpr (!DENSE) rm[u] = *reinterpret_cast<const u32x2*>(pm + static_cast<int64_t>(kt) * 128);
-#pragma unroll
-            for (int s4 = 0; s4 < 4; ++s4)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const int64_t k = static_cast<int64_t>(kt) * SK + 64 * c + 16 * s4 + 8 * h;
-                    if constexpr (GUARD) {
-                        b[u][s4].q[c] = load_guarded(row, k, K);
-                    } else {                                                     // K is a multiple of 8: whole granules, or none
-                        const u32x4 v = *reinterpret_cast<const u32x4*>(row + (k < K ? k : 0));
-                        b[u][s4].q[c] = k < K ? v : (u32x4){0u, 0u, 0u, 0u};
-                    }
-                }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (st + u * NW < nk) {
-#pragma unroll
-                for (int s4 = 0; s4 < 4; ++s4) {
-                    if constexpr (DENSE) {
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            AFrag af, bh;
-                            af.q = ra[u][2 * s4 + x];
-                            bh.q = b[u][s4].q[x];
-                            acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af.v, bh.v, acc[0][0], 0, 0, 0);
-                        }
-                    } else {
-                        AFrag af;
-                        af.q = ra[u][s4];
-                        const int idx = static_cast<int>(s4 < 2 ? rm[u].x : rm[u].y);
-                        if (s4 & 1) acc[0][0] = __builtin_amdgcn_smfmac_f32_32x32x32_bf16(af.v, b[u][s4].v, acc[0][0], idx, 0, 1);
-                        else acc[0][0] = __builtin_amdgcn_smfmac_f32_32x32x32_bf16(af.v, b[u][s4].v, acc[0][0], idx, 0, 0);
-                    }
-                }
-            }
-    }
-    if (wave > 0)
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            part[((wave - 1) * 4 + q) * 64 + lane] = (f32x4){acc[0][0][4 * q], acc[0][0][4 * q + 1], acc[0][0][4 * q + 2], acc[0][0][4 * q + 3]};
-    __syncthreads();
-    if (wave == 0)
-#pragma unroll
-        for (int w = 0; w < NW - 1; ++w)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const f32x4 x = part[(w * 4 + q) * 64 + lane];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[0][0][4 * q + e] += x[e];
-            }
-    __syncthreads();
-    out.finish<32, 32, 32, 32, 1, 1, 64 * NW>(acc, reinterpret_cast<uint8_t*>(part), wave == 0, 0, 0, lane, rt * 32, t0, Adim, T, C, ldc, vecC);
+template <int TN, bool DENSE>
+__global__ void __launch_bounds__(64 * kWideWaves, 2)
+k_linear_wide(const uint16_t* __restrict__ A, const uint32_t* __restrict__ Ameta, int Adim, int K, const uint16_t* __restrict__ Bsrc, int64_t ldb,
+              int64_t T, uint16_t* C, int64_t ldc, int rpt, int wpp, bool stream_out, LinearOut out) {
+    gemm_sp24_wide_body<TN, DENSE>(A, Ameta, Adim, K, Bsrc, ldb, nullptr, T, C, ldc, rpt, wpp, stream_out, out);
 }
 
 template <bool SPARSE, int NW, int R>
@@ -113,10 +42,10 @@ struct Problem {
     const void* A; const uint32_t* meta; int64_t Adim, K; const void* Bm; int64_t T, ldb; void* C; int64_t ldc; hipStream_t s;
 };
 
-template <int BM, int BN, int WAVES_M, int WAVES_N, int KG, int PF, bool BGUARD, bool BHALF, bool KTAIL, bool DENSE>
+template <int BM, int BN, int WAVES_M, int WAVES_N, int KG, int PF, bool BGUARD, bool BHALF, bool KTAIL, bool DENSE, int TR = BN>
 int run_t(const Problem& p, const LinearOut& out) {
     using S = SpSmem<BN, KG>;
-    auto kern = k_linear_sp24<BM, BN, WAVES_M, WAVES_N, KG, PF, BGUARD, BHALF, KTAIL, DENSE>;
+    auto kern = k_linear_sp24<BM, BN, WAVES_M, WAVES_N, KG, PF, BGUARD, BHALF, KTAIL, DENSE, TR>;
     if (S::kTotal > 48 * 1024) {
         static DeviceMemo attr_set;
         const int dev = DeviceMemo::device();
@@ -134,6 +63,7 @@ int run_t(const Problem& p, const LinearOut& out) {
     return check_launch();
 }
 
+// (TR: token rows fetched, where the tile has more than there are)
 // rows: 0 whole stages of 16-byte token rows, 1 the last stage may end early (K a multiple of 8), 2 any rows (4-byte loads)
 template <int BM, int BN, int WAVES_M, int WAVES_N, int PF, bool BHALF, int KG, bool DENSE>
 int run(const Problem& p, const LinearOut& out, int rows) {
@@ -142,12 +72,49 @@ int run(const Problem& p, const LinearOut& out, int rows) {
     return run_t<BM, BN, WAVES_M, WAVES_N, KG, 1, true, false, false, DENSE>(p, out);
 }
 
-template <bool GUARD, bool DENSE>
-int run_few(const Problem& p, const LinearOut& out) {
-    if (ceil_div(p.Adim, 32) * (64 * kFewWaves) > 0xFFFFFFFFll) return BIMASK_ERR_SHAPE;
-    const dim3 grid(static_cast<unsigned>(ceil_div(p.Adim, 32)), static_cast<unsigned>(ceil_div(p.T, 32)));
-    hipLaunchKernelGGL((k_linear_few<GUARD, DENSE>), grid, dim3(64 * kFewWaves), 0, p.s, static_cast<const uint16_t*>(p.A), p.meta, p.Adim, p.K,
-                       static_cast<const uint16_t*>(p.Bm), p.T, p.ldb, static_cast<uint16_t*>(p.C), p.ldc, aligned16(p.C) && p.ldc % 8 == 0, out);
+template <int TN, bool DENSE>
+int run_wide(const Problem& p, const LinearOut& out, const WidePlan& w) {
+    static DeviceMemo attr_set;
+    const int dev = DeviceMemo::device();
+    auto kern = k_linear_wide<TN, DENSE>;
+    if (!attr_set.get(dev)) {
+        if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kWideLds) != hipSuccess)
+            return BIMASK_ERR_HIP;
+        attr_set.set(dev, 1);
+    }
+    hipLaunchKernelGGL(kern, dim3(w.grid, w.pieces), dim3(64 * kWideWaves), w.lds, p.s, static_cast<const uint16_t*>(p.A), p.meta,
+                       static_cast<int>(p.Adim), static_cast<int>(p.K), static_cast<const uint16_t*>(p.Bm), p.ldb, p.T,
+                       static_cast<uint16_t*>(p.C), p.ldc, w.rpt, w.wpp, streams_out(p.C, p.Adim, p.ldc, false), out);
+    return check_launch();
+}
+
+// Short contractions and wide outputs: the epilogue is most of the work there, and in this kernel it is each wavefront's own.
+template <bool DENSE>
+int run_short(const Problem& p, const LinearOut& out) {
+    if (p.K > 512 || p.K % 8 || p.Adim % 8 || p.Adim <= 256 || p.T < 2048 || p.T > 0x7FFFFFFF || p.ldc >= (1 << 28)) return BIMASK_ERR_UNSUPPORTED;
+    if (!aligned16(p.Bm) || !aligned16(p.C) || p.ldb % 8 || p.ldc % 8 || (out.R && !out.vecR)) return BIMASK_ERR_UNSUPPORTED;
+    WidePlan p2, p4;
+    const double us2 = wide_plan(2, p.Adim, p.K, p.T, false, DENSE, p2), us4 = wide_plan(4, p.Adim, p.K, p.T, false, DENSE, p4);
+    if (us2 == 0) return BIMASK_ERR_UNSUPPORTED;
+    return us4 != 0 && us4 < us2 ? run_wide<4, DENSE>(p, out, p4) : run_wide<2, DENSE>(p, out, p2);
+}
+
+// the largest problems, on conditions of launch_gemm_sp24_big
+int run_big(const Problem& p, const LinearOut& out) {
+    if (!gemm_sp24_big_shape(p.Adim, p.K, p.T) || !aligned16(p.Bm) || !aligned16(p.C) || p.ldb % 8 || p.ldc % 8) return BIMASK_ERR_UNSUPPORTED;
+    const int64_t tiles_a = ceil_div(p.Adim, kBigRows), tiles_t = ceil_div(p.T, kBigTokens);
+    if (round_up(p.Adim, 32) * (p.K / 2) > 0x7FFFFFFFll || p.T * p.ldb + p.K > 0x7FFFFFFFll || tiles_t * tiles_a > 0x0FFFFFFFll)
+        return BIMASK_ERR_UNSUPPORTED;
+    static DeviceMemo attr_set;
+    const int dev = DeviceMemo::device();
+    if (!attr_set.get(dev)) {
+        if (hipFuncSetAttribute(reinterpret_cast<const void*>(k_linear_sp24_big), hipFuncAttributeMaxDynamicSharedMemorySize, kBigSmem) != hipSuccess)
+            return BIMASK_ERR_HIP;
+        attr_set.set(dev, 1);
+    }
+    hipLaunchKernelGGL(k_linear_sp24_big, dim3(256), dim3(kBigThreads), kBigSmem, p.s, static_cast<const uint16_t*>(p.A), p.meta, p.Adim,
+                       static_cast<int>(p.K / 128), static_cast<const uint16_t*>(p.Bm), p.T, p.ldb, static_cast<uint16_t*>(p.C), p.ldc,
+                       static_cast<int>(tiles_a), static_cast<int>(tiles_t), static_cast<int>(ceil_div(tiles_t, 8)), out);
     return check_launch();
 }
 
@@ -182,9 +149,29 @@ template <bool DENSE>
 int run_bf16(const Problem& p, const LinearOut& out) {
     const bool rows16 = aligned16(p.Bm) && p.ldb % 8 == 0 && p.K % 8 == 0;
     const int rows = !rows16 ? 2 : p.K % SK == 0 ? 0 : 1;
-    if (p.T <= 32) return rows == 2 ? run_few<true, DENSE>(p, out) : run_few<false, DENSE>(p, out);
-    const bool split32 = p.K > (rows16 ? 256 : 384) && gemm_few_tiles(p.Adim, p.T);
-    if (split32) return run<64, 32, 2, 1, 1, false, 4, DENSE>(p, out, rows);
+    if (const int rc = run_short<DENSE>(p, out); rc != BIMASK_ERR_UNSUPPORTED) return rc;
+    if constexpr (!DENSE) {
+        const int rc = run_big(p, out);
+        if (rc != BIMASK_ERR_UNSUPPORTED) return rc;
+    }
+    // Long contractions with few tiles: split inside the workgroup.  2-of-4: one 32 x 32 tile on eight wavefronts where such tiles are
+    // one per CU at most (serving: the weights are read once, and CUs without a tile read none), with as many stages in flight as the
+    // token rows leave registers for (4096 x 4096 at one token 5.7 us, with 64 x 32 tiles 8.6; 4096 x 11008 at 13 12.5 / 17.6).
+    const bool deep = p.K > (rows16 ? 256 : 384);
+    if constexpr (!DENSE)
+        if (p.K > 2048 && ceil_div(p.Adim, 32) * ceil_div(p.T, 32) <= 256) {
+            if (rows == 2) return run_t<32, 32, 1, 1, 8, 1, true, false, false, false>(p, out);
+            if (p.T <= 4) return run_t<32, 32, 1, 1, 8, 3, false, false, true, false, 4>(p, out);
+            if (p.T <= 16) return run_t<32, 32, 1, 1, 8, 2, false, false, true, false, 16>(p, out);
+            return run_t<32, 32, 1, 1, 8, 1, false, false, true, false>(p, out);
+        }
+    if (deep && gemm_few_tiles(p.Adim, p.T)) {
+        if constexpr (!DENSE) return run<64, 32, 2, 1, 1, false, 4, false>(p, out, rows);
+        // (the form for whole stages would not fit the registers)
+        else return rows == 2 ? run_t<64, 32, 2, 1, 4, 1, true, false, false, true>(p, out) : run_t<64, 32, 2, 1, 4, 1, false, false, true, true>(p, out);
+    }
+    if constexpr (!DENSE)
+        if (deep && p.Adim > 64 && ceil_div(p.Adim, 64) * ceil_div(p.T, 64) <= 256) return run<64, 64, 2, 2, 1, false, 2, false>(p, out, rows);
     if (p.Adim <= 64) return run<64, 64, 2, 2, 2, false, 1, DENSE>(p, out, rows);
     const int64_t w256 = round_up(p.Adim, 256), w128 = round_up(p.Adim, 128);
     const bool narrow = (w256 - w128) * 5 >= w256, big = ceil_div(p.Adim, 256) * ceil_div(p.T, 128) >= 190;

@@ -15,143 +15,197 @@ struct LinearOut {                                       // bf16
     bool vecR;                                           // rows of R start on 16 bytes
     static constexpr bool kFused = true;
 
-    // Sums of a workgroup's tile, BM weight rows x BN tokens: a wavefront that is `mine` holds TM x TN accumulators of 32 rows x 32
-    // tokens at row WM wm, token WN wn; lane (l32, h) has token l32 and rows 8 q + 4 h + 0..3 in quad q.  A block of the checkpoint is
-    // one accumulator's rows of one token: two lanes, so its maximum takes one exchange and no LDS.  Codes, residual and output go
-    // through LDS (smem: 2 BM BN bytes at least) and leave or arrive as whole row segments of the tile; the residual waits in the
-    // place of the output piece it is added to.
-    // Adim is a multiple of 4, so quads are inside or outside; sums beyond it may be NaN and count as 0 in the checkpoint.
-    template <int BM, int BN, int WM, int WN, int TM, int TN, int NT, class ACC>
-    __device__ __forceinline__ void finish(ACC (&acc)[TM][TN], uint8_t* smem, bool mine, int wm, int wn, int lane, int64_t a0, int64_t t0,
+    // Sums of a workgroup's tile, BM weight rows x BN tokens.  Wavefront (wm, wn) holds TM x TN accumulators of 32 rows x 32 tokens from
+    // row WM wm, token WN wn on (lane (l32, h): token l32, rows 8 q + 4 h + 0..3 in quad q); with KG > 1 group kg holds a share of every
+    // sum.  They go to LDS as fp32 (smem: 4 KG BN BM / PASSES bytes, BM / PASSES rows at a time; 16-byte chunks XOR-swizzled by the token), and
+    // every thread then takes 8 consecutive features of a token at a time: residual and output move as whole row segments, a block of
+    // the checkpoint is four neighbouring lanes, the groups' shares are added in group order.
+    // Adim is a multiple of 4, so a piece's halves are inside or outside; sums beyond it may be NaN and count as 0 in the checkpoint.
+    template <int BM, int BN, int WM, int WN, int TM, int TN, int NT, int KG, int PASSES, class ACC>
+    __device__ __forceinline__ void finish(ACC (&acc)[TM][TN], uint8_t* smem, int kg, int wm, int wn, int lane, int64_t a0, int64_t t0,
                                            int64_t Adim, int64_t T, uint16_t* C, int64_t ldc, bool vecC) const {
         typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
         typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-        const int l32 = lane & 31, h = lane >> 5, tid = threadIdx.x;
-        const int64_t ar = a0 + wm * WM + 4 * h;         // this lane's first row
-        if (bias && mine)
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int64_t a = ar + 32 * i + 8 * q;
-                    u32x2 b = {0u, 0u};
-                    if (a < Adim) b = *reinterpret_cast<const u32x2*>(bias + a);
-#pragma unroll
-                    for (int j = 0; j < TN; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            acc[i][j][4 * q + e] += __builtin_bit_cast(float, e & 1 ? b[e >> 1] & 0xFFFF0000u : b[e >> 1] << 16);
-                }
-        if (codes) {
-            constexpr int UPR = BM / 16;                 // 16-byte units of a token's codes in the tile
-            uint8_t* sScale = smem + BM * BN;
-            if (mine)
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
+        constexpr int ROWS = BM / PASSES, UPR = ROWS / 8;            // features of a token in a pass, pieces of 8
+        static_assert(ROWS % WM == 0, "a pass takes whole wavefronts");
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(lane), "+v"(tid));        // (what depends on them is not kept across the caller's loop)
+        f32x4* sums = reinterpret_cast<f32x4*>(smem);
+        auto chunk = [](int g, int t, int c) { return (g * BN + t) * (ROWS / 4) + (c ^ (t & (ROWS < 64 ? 7 : 15))); };
+        const int64_t pitch = ckpt_pitch(Adim);
+#pragma unroll 1
+        for (int pass = 0; pass < PASSES; ++pass) {
+            if (pass > 0) __syncthreads();               // the previous pass has been read
+            if (PASSES == 1 || wm * WM / ROWS == pass)
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) {
-                        float z[16];
-                        uint32_t most = 0;
+                    for (int j = 0; j < TN; ++j)
 #pragma unroll
-                        for (int q = 0; q < 16; ++q) {
-                            z[q] = ar + 32 * i + 8 * (q >> 2) < Adim ? acc[i][j][q] : 0.f;
-                            const uint32_t m = __builtin_bit_cast(uint32_t, z[q]) & 0x7FFFFFFFu;
-                            most = m > most ? m : most;
-                        }
-                        const auto both = __builtin_amdgcn_permlane32_swap(most, most, false, false);
-                        const int byte = ckpt_scale_byte(both[0] > both[1] ? both[0] : both[1]);
-                        const bool bad = byte == kCkptNaN;
-                        const float inv = ckpt_inverse(bad ? 127 : byte);
-                        uint32_t d[4];
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) d[q] = ckpt_codes(z + 4 * q, inv, bad);
-                        const auto lo = __builtin_amdgcn_permlane32_swap(d[0], d[2], false, false);
-                        const auto hi = __builtin_amdgcn_permlane32_swap(d[1], d[3], false, false);
-                        const int t = wn * WN + 32 * j + l32, u = (wm * WM + 32 * i) / 16 + h;
-                        *reinterpret_cast<u32x4*>(smem + t * BM + ((u ^ (t & (UPR - 1))) << 4)) = (u32x4){lo[0], lo[1], hi[0], hi[1]};
-                        if (h == 0) sScale[t * (BM / 32) + wm * (WM / 32) + i] = static_cast<uint8_t>(byte);
-                    }
+                        for (int q = 0; q < 4; ++q)
+                            sums[chunk(kg, wn * WN + 32 * j + (lane & 31), (wm * WM % ROWS + 32 * i) / 4 + 2 * q + (lane >> 5))] =
+                                (f32x4){acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
             __syncthreads();
-            const int64_t pitch = ckpt_pitch(Adim), blocks = ckpt_blocks(Adim);
-            for (int q = tid; q < BN * UPR; q += NT) {
+            const int n_tok = static_cast<int>(T - t0 < BN ? T - t0 : BN);
+#pragma unroll 1
+            for (int q = tid; q < n_tok * UPR; q += NT) {
                 const int t = q / UPR, u = q % UPR;
-                if (t0 + t < T && a0 + 16 * u < pitch)
-                    *reinterpret_cast<u32x4*>(codes + (t0 + t) * pitch + a0 + 16 * u) =
-                        *reinterpret_cast<const u32x4*>(smem + t * BM + ((u ^ (t & (UPR - 1))) << 4));
-            }
-            for (int q = tid; q < BN * (BM / 32); q += NT) {
-                const int t = q / (BM / 32), b = q % (BM / 32);
-                if (t0 + t < T && a0 / 32 + b < blocks) scales[(t0 + t) * blocks + a0 / 32 + b] = sScale[q];
-            }
-            __syncthreads();
-        }
-        constexpr int UPR = BM / 8;                      // 16-byte units of a token's outputs in the tile
-        if (R) {
-            for (int q = tid; q < BN * UPR; q += NT) {
-                const int t = q / UPR, u = q % UPR;
-                const int64_t a = a0 + 8 * u;
-                u32x4 v = {0u, 0u, 0u, 0u};
-                if (t0 + t < T && a < Adim) {
+                const int64_t a = a0 + pass * ROWS + 8 * u;
+                const bool in0 = a < Adim, in1 = a + 4 < Adim;
+                u32x4 r = {0u, 0u, 0u, 0u};
+                if (R && in0) {
                     const uint16_t* src = R + (t0 + t) * ldr + a;
-                    if (vecR && a + 8 <= Adim) {
-                        v = *reinterpret_cast<const u32x4*>(src);
+                    if (vecR && in1) {
+                        r = *reinterpret_cast<const u32x4*>(src);
                     } else {                             // 4-byte pieces (pointer and pitch are 4-byte aligned, Adim even)
 #pragma unroll
                         for (int d = 0; d < 4; ++d)
-                            if (a + 2 * d < Adim) v[d] = *reinterpret_cast<const uint32_t*>(src + 2 * d);
+                            if (d < 2 || in1) r[d] = *reinterpret_cast<const uint32_t*>(src + 2 * d);
                     }
                 }
-                *reinterpret_cast<u32x4*>(smem + t * (BM * 2) + ((u ^ ((2 * t) & (UPR - 1))) << 4)) = v;
-            }
-            __syncthreads();
-        }
-        if (mine)
+                u32x4 b = {0u, 0u, 0u, 0u};
+                if (bias) {
+                    if (in0) *reinterpret_cast<u32x2*>(&b) = *reinterpret_cast<const u32x2*>(bias + a);
+                    if (in1) reinterpret_cast<u32x2*>(&b)[1] = *reinterpret_cast<const u32x2*>(bias + a + 4);
+                }
+                float z[8];
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+                for (int c = 0; c < 2; ++c) {
+                    f32x4 x = sums[chunk(0, t, 2 * u + c)];
 #pragma unroll
-                for (int j = 0; j < TN; ++j) {
-                    const int t = wn * WN + 32 * j + l32;
-                    float y[16];
+                    for (int g = 1; g < KG; ++g) x += sums[chunk(g, t, 2 * u + c)];
 #pragma unroll
-                    for (int q = 0; q < 16; ++q) y[q] = acc[i][j][q];
-                    apply_act(y, act);
+                    for (int e = 0; e < 4; ++e)
+                        z[4 * c + e] = x[e] + __builtin_bit_cast(float, e & 1 ? b[2 * c + (e >> 1)] & 0xFFFF0000u : b[2 * c + (e >> 1)] << 16);
+                }
+                if (codes) {
+                    float v[8];
+                    uint32_t most = 0, d[2];
 #pragma unroll
-                    for (int p = 0; p < 2; ++p) {
-                        const int u = (wm * WM + i * 32 + 16 * p + 8 * h) >> 3;
-                        u32x4* unit = reinterpret_cast<u32x4*>(smem + t * (BM * 2) + ((u ^ ((2 * t) & (UPR - 1))) << 4));
-                        if (R) {                         // the exchange below, backwards: the pairs that this lane's quads are added to
-                            const u32x4 r = *unit;
-                            const auto rlo = __builtin_amdgcn_permlane32_swap(r.x, r.z, false, false);
-                            const auto rhi = __builtin_amdgcn_permlane32_swap(r.y, r.w, false, false);
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                y[8 * p + 4 * e + 0] += __builtin_bit_cast(float, static_cast<uint32_t>(rlo[e]) << 16);
-                                y[8 * p + 4 * e + 1] += __builtin_bit_cast(float, static_cast<uint32_t>(rlo[e]) & 0xFFFF0000u);
-                                y[8 * p + 4 * e + 2] += __builtin_bit_cast(float, static_cast<uint32_t>(rhi[e]) << 16);
-                                y[8 * p + 4 * e + 3] += __builtin_bit_cast(float, static_cast<uint32_t>(rhi[e]) & 0xFFFF0000u);
-                            }
-                        }
-                        const auto slo = __builtin_amdgcn_permlane32_swap(pack_bf16(y[8 * p + 0], y[8 * p + 1]), pack_bf16(y[8 * p + 4], y[8 * p + 5]), false, false);
-                        const auto shi = __builtin_amdgcn_permlane32_swap(pack_bf16(y[8 * p + 2], y[8 * p + 3]), pack_bf16(y[8 * p + 6], y[8 * p + 7]), false, false);
-                        *unit = (u32x4){slo[0], shi[0], slo[1], shi[1]};
+                    for (int e = 0; e < 8; ++e) {
+                        v[e] = (e < 4 ? in0 : in1) ? z[e] : 0.f;
+                        const uint32_t m = __builtin_bit_cast(uint32_t, v[e]) & 0x7FFFFFFFu;
+                        most = m > most ? m : most;
+                    }
+                    uint32_t o = __builtin_amdgcn_mov_dpp(most, 0xB1, 0xF, 0xF, true);       // the other lane of a pair, the other pair of four
+                    most = o > most ? o : most;
+                    o = __builtin_amdgcn_mov_dpp(most, 0x4E, 0xF, 0xF, true);
+                    most = o > most ? o : most;
+                    const int byte = ckpt_scale_byte(most);
+                    ckpt_encode(v, byte, d);
+                    if (a < pitch) {
+                        *reinterpret_cast<u32x2*>(codes + (t0 + t) * pitch + a) = (u32x2){d[0], d[1]};
+                        if ((u & 3) == 0) scales[(t0 + t) * (pitch / 32) + a / 32] = static_cast<uint8_t>(byte);
                     }
                 }
-        __syncthreads();
-        for (int q = tid; q < BN * UPR; q += NT) {
-            const int t = q / UPR, u = q % UPR;
-            const u32x4 v = *reinterpret_cast<const u32x4*>(smem + t * (BM * 2) + ((u ^ ((2 * t) & (UPR - 1))) << 4));
-            const int64_t a = a0 + 8 * u;
-            if (t0 + t < T && a < Adim) {
-                uint16_t* dst = C + (t0 + t) * ldc + a;
-                if (vecC && a + 8 <= Adim) {
-                    __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(dst));
-                } else {
+                apply_act<true>(z, act);
+                u32x4 y;
 #pragma unroll
-                    for (int d = 0; d < 4; ++d)
-                        if (a + 2 * d < Adim) reinterpret_cast<uint32_t*>(dst)[d] = v[d];
+                for (int d = 0; d < 4; ++d) {
+                    const float lo = __builtin_bit_cast(float, r[d] << 16), hi = __builtin_bit_cast(float, r[d] & 0xFFFF0000u);
+                    y[d] = R ? pack_bf16(z[2 * d] + lo, z[2 * d + 1] + hi) : pack_bf16(z[2 * d], z[2 * d + 1]);
+                }
+                if (in0) {
+                    uint16_t* dst = C + (t0 + t) * ldc + a;
+                    if (vecC && in1) {
+                        __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(dst));
+                    } else {
+#pragma unroll
+                        for (int d = 0; d < 4; ++d)
+                            if (d < 2 || in1) reinterpret_cast<uint32_t*>(dst)[d] = y[d];
+                    }
                 }
             }
         }
+    }
+
+    // The same within one wavefront, on two accumulators (64 weight rows from a0 x 32 tokens from t0, `rows` of which exist) before they
+    // are rounded: bias, checkpoint, activation and residual.  strip: 32 rows of 136 bytes of the wavefront's own.
+    // `ahead`: with AHEAD this residual piece, requested before (fetch_residual), replaced by the next one's if there is one.
+    typedef unsigned int Piece __attribute__((ext_vector_type(4)));
+    __device__ __forceinline__ void fetch_residual(Piece (&ahead)[4], int lane, int a0, int64_t t0, int rows, int Adim) const {
+        if (!R) return;
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {                 // beyond the tile: loaded from its first piece, not used
+            const int r = (lane >> 3) + 8 * it, c = 8 * (lane & 7);
+            ahead[it] = *reinterpret_cast<const Piece*>(R + (t0 + (r < rows ? r : 0)) * ldr + a0 + (c < Adim - a0 ? c : 0));      // Adim is a multiple of 8
+        }
+    }
+    template <bool AHEAD, class ACC>
+    __device__ __forceinline__ void before_rounding(ACC& z0, ACC& z1, Piece (&ahead)[4], bool more, uint8_t* strip, int lane, int a0, int64_t t0, int rows,
+                                                    int Adim) const {
+        typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+        typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+        asm volatile("" : "+v"(lane));                   // (what depends on it is not kept across the caller's loop)
+        const int l32 = lane & 31, h = lane >> 5;
+        const int64_t t = t0 + l32;
+        if constexpr (!AHEAD) fetch_residual(ahead, lane, a0, t0, rows, Adim);
+        if (R) {                                         // as whole row segments into the strip
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                u32x2* d = reinterpret_cast<u32x2*>(strip + ((lane >> 3) + 8 * it) * 136 + 16 * (lane & 7));
+                d[0] = (u32x2){ahead[it].x, ahead[it].y};
+                d[1] = (u32x2){ahead[it].z, ahead[it].w};
+            }
+            if (AHEAD && more) fetch_residual(ahead, lane, a0, t0 + 32, rows - 32, Adim);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        auto half = [&](ACC& z, int i) {
+            float y[16];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int a = a0 + 32 * i + 8 * q + 4 * h;
+                u32x2 b = {0u, 0u};
+                if (bias && a < Adim) b = *reinterpret_cast<const u32x2*>(bias + a);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    y[4 * q + e] = z[4 * q + e] + __builtin_bit_cast(float, e & 1 ? b[e >> 1] & 0xFFFF0000u : b[e >> 1] << 16);
+            }
+            if (codes && a0 + 32 * i < Adim) {
+                float v[16];
+                uint32_t most = 0, d[4];
+#pragma unroll
+                for (int q = 0; q < 16; ++q) {
+                    v[q] = a0 + 32 * i + 8 * (q >> 2) + 4 * h < Adim ? y[q] : 0.f;
+                    const uint32_t m = __builtin_bit_cast(uint32_t, v[q]) & 0x7FFFFFFFu;
+                    most = m > most ? m : most;
+                }
+                const auto both = __builtin_amdgcn_permlane32_swap(most, most, false, false);
+                const int byte = ckpt_scale_byte(both[0] > both[1] ? both[0] : both[1]);
+                ckpt_encode(v, byte, d);
+                const auto lo = __builtin_amdgcn_permlane32_swap(d[0], d[2], false, false);
+                const auto hi = __builtin_amdgcn_permlane32_swap(d[1], d[3], false, false);
+                if (l32 < rows) {
+                    const int64_t pitch = ckpt_pitch(Adim);
+                    *reinterpret_cast<u32x4*>(codes + t * pitch + a0 + 32 * i + 16 * h) = (u32x4){lo[0], lo[1], hi[0], hi[1]};
+                    if (h == 0) scales[t * (pitch / 32) + a0 / 32 + i] = static_cast<uint8_t>(byte);
+                }
+            }
+            apply_act<true>(y, act);
+            if (R) {
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const u32x2* d = reinterpret_cast<const u32x2*>(strip + l32 * 136 + 2 * (32 * i + 16 * p + 8 * h));
+                    const u32x2 r0 = d[0], r1 = d[1];
+                    const auto rlo = __builtin_amdgcn_permlane32_swap(r0.x, r1.x, false, false);
+                    const auto rhi = __builtin_amdgcn_permlane32_swap(r0.y, r1.y, false, false);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        y[8 * p + 4 * e + 0] += __builtin_bit_cast(float, static_cast<uint32_t>(rlo[e]) << 16);
+                        y[8 * p + 4 * e + 1] += __builtin_bit_cast(float, static_cast<uint32_t>(rlo[e]) & 0xFFFF0000u);
+                        y[8 * p + 4 * e + 2] += __builtin_bit_cast(float, static_cast<uint32_t>(rhi[e]) << 16);
+                        y[8 * p + 4 * e + 3] += __builtin_bit_cast(float, static_cast<uint32_t>(rhi[e]) & 0xFFFF0000u);
+                    }
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 16; ++q) z[q] = y[q];
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        half(z0, 0);
+        half(z1, 1);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 };
 
@@ -177,17 +231,17 @@ struct LinearOutF32 {
                 most = o > most ? o : most;
             }
             const int byte = ckpt_scale_byte(most);
-            const bool bad = byte == kCkptNaN;
-            const float v4[4] = {v, 0.f, 0.f, 0.f};
-            const uint32_t code = ckpt_codes(v4, ckpt_inverse(bad ? 127 : byte), bad);
+            float v4[4] = {v, 0.f, 0.f, 0.f};
+            uint32_t code[1];
+            ckpt_encode(v4, byte, code);
             const int64_t pitch = ckpt_pitch(Adim);
             if (t < T && a < pitch) {
-                codes[t * pitch + a] = static_cast<uint8_t>(code);
+                codes[t * pitch + a] = static_cast<uint8_t>(code[0]);
                 if ((a & 31) == 0) scales[t * (pitch / 32) + a / 32] = static_cast<uint8_t>(byte);
             }
         }
         if (in) {
-            apply_act(z, act);
+            apply_act<false>(z, act);
             C[t * ldc + a] = R ? z[0] + R[t * ldr + a] : z[0];
         }
     }
