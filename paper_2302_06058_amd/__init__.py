@@ -108,13 +108,14 @@ def _nbytes(t) -> int:
 # The step of a small layer is bound by the host: five calls with a launch or two of 3.3 us each.  What a wrapper adds to its
 # launches counts as much: torch.cuda.current_stream() builds a Stream object (2.8 us), the handle behind it costs 0.1 us.
 # With that and new_empty (1.4 us against 1.7) a wrapper went from 5.0-7.2 us beyond its launches to 2-3.
-_raw_stream = _device_index = None
+_raw_stream = _device_index = _torch = None
 
 
 def _bind_stream() -> None:
     """Where to ask for the current stream's handle (torch is imported at the first call, not with this module)."""
-    global _raw_stream, _device_index
+    global _raw_stream, _device_index, _torch
     import torch
+    _torch = torch
     torch.cuda.current_stream()                          # initialises the runtime
     try:
         from torch._C import _cuda_getCurrentRawStream as raw, _cuda_getDevice as index
@@ -384,42 +385,54 @@ def checkpoint_bytes(T: int, cols: int) -> int:
     return int(lib().bimask_checkpoint_bytes(T, cols))
 
 
-def _on_current_device(*ts):
+def _on_current_device(*ts) -> None:
     """The calls below enqueue on the current device's stream: tensors of another device are refused."""
-    _need_cuda(*ts)
     if _device_index is None:
+        _need_cuda(*ts)
         _bind_stream()
     d = _device_index()
     for t in ts:
         if t is not None and t.get_device() != d:
+            _need_cuda(t)
             raise ValueError("all tensors must live on the current device")
 
 
 def _pitch(t) -> int:
     """Leading dimension of a matrix with unit stride along its rows; of a single row it is no stride that anyone steps by."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] != 1):
+    rows, cols = t.shape
+    return _pitch_of(t, rows, cols)
+
+
+def _pitch_of(t, rows: int, cols: int) -> int:
+    ld, unit = t.stride()
+    if unit != 1 and cols != 1:
         raise ValueError("expected a 2-D tensor with unit stride along its last dimension")
-    return t.stride(0) if t.shape[0] != 1 else (t.shape[1] + 7) // 8 * 8
+    return ld if rows != 1 else (cols + 7) // 8 * 8
 
 
-def _expect(t, name: str, shape, dtype) -> None:
-    if t is not None and (tuple(t.shape) != shape or t.dtype != dtype):
-        raise ValueError(f"{name} must be a {' x '.join(map(str, shape))} tensor of {dtype}")
+def _rows_of(t, name: str, rows: int, cols: int, dtype) -> int:
+    """Leading dimension of a rows x cols matrix of `dtype`."""
+    if t.shape != (rows, cols) or t.dtype != dtype:
+        raise ValueError(f"{name} must be a {rows} x {cols} tensor of {dtype}")
+    return _pitch_of(t, rows, cols)
+
+
+def _vector(t, name: str, n: int, dtype) -> None:
+    if t.shape != (n,) or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor of {n} entries of {dtype}")
 
 
 def _ckpt_buffer(ckpt, T: int, cols: int, like):
-    import torch
     if ckpt is None:
-        return _empty((checkpoint_bytes(T, cols),), torch.uint8, like)
-    if ckpt.dtype != torch.uint8 or not ckpt.is_contiguous():
+        return _empty((T * ((cols + 31) // 32 * 33),), _torch.uint8, like)
+    if ckpt.element_size() != 1 or not ckpt.is_contiguous():
         raise ValueError("a checkpoint is a contiguous uint8 tensor")
     return ckpt
 
 
 def _workspace(workspace, need: int, like):
     if workspace is None and need:
-        import torch
-        return _empty((need,), torch.uint8, like)
+        return _empty((need,), _torch.uint8, like)
     return workspace
 
 
@@ -430,20 +443,20 @@ def bimask_checkpoint_store(X, ckpt=None):
     T, C = X.shape
     ckpt = _ckpt_buffer(ckpt, T, C, X)
     _check("bimask_checkpoint_store",
-           lib().bimask_checkpoint_store(_ptr(X), T, C, ldx, _dtype_code(X), _ptr(ckpt), _nbytes(ckpt), _stream()))
+           lib().bimask_checkpoint_store(X.data_ptr(), T, C, ldx, _dtype_code(X), ckpt.data_ptr(), ckpt.numel(), _stream()))
     return ckpt
 
 
 def bimask_checkpoint_load(ckpt, T: int, C: int, dtype=None, X=None):
     """The values that a checkpoint stands for, T x C in `dtype` (torch.bfloat16 if neither it nor X says otherwise)."""
-    import torch
     _on_current_device(ckpt, X)
     _ckpt_buffer(ckpt, T, C, ckpt)
     if X is None:
-        X = _empty((T, C), dtype or torch.bfloat16, ckpt)
-    _expect(X, "X", (T, C), dtype or X.dtype)
+        X, ldx = _empty((T, C), dtype or _torch.bfloat16, ckpt), C
+    else:
+        ldx = _rows_of(X, "X", T, C, dtype or X.dtype)
     _check("bimask_checkpoint_load",
-           lib().bimask_checkpoint_load(_ptr(ckpt), _nbytes(ckpt), T, C, _dtype_code(X), _ptr(X), _pitch(X), _stream()))
+           lib().bimask_checkpoint_load(ckpt.data_ptr(), ckpt.numel(), T, C, _dtype_code(X), X.data_ptr(), ldx, _stream()))
     return X
 
 
@@ -451,51 +464,52 @@ def bimask_sparse_linear_fwd(X, Wf_values, Wf_index, I: int, J: int, N: int, M: 
                              Y=None, ckpt=None, want_ckpt: bool = False):
     """Y = act(Z) + residual with Z = X (B .* W)^T + bias; returns (Y, checkpoint of Z or None).  residual may be Y itself."""
     _on_current_device(X, Wf_values, Wf_index, bias, residual, Y, ckpt)
-    ldx = _pitch(X)
-    T = X.shape[0]
-    _expect(X, "X", (T, J), X.dtype)
-    if Wf_values.dtype != X.dtype or Wf_values.numel() < operand_elems(I, J, N, M):
+    T, dtype = X.shape[0], X.dtype
+    ldx = _rows_of(X, "X", T, J, dtype)
+    code = _dtype_code(X)
+    slots = (I + 31) // 32 * ((J + 127) // 128) * 2048               # slot values of a 2-of-4 operand, a sixteenth as many index words
+    if Wf_values.dtype != dtype or Wf_values.numel() < (slots if N <= 2 else 2 * slots):
         raise ValueError("Wf_values must hold the operand of an I x J matrix in the type of X")
-    if Wf_index is not None and Wf_index.numel() < operand_index_words(I, J, N, M):
+    if N <= 2 and Wf_index is not None and Wf_index.numel() * 16 < slots:
         raise ValueError("Wf_index must hold the index words of an I x J matrix")
-    _expect(bias, "bias", (I,), X.dtype)
-    if bias is not None and not bias.is_contiguous():
-        raise ValueError("bias must be contiguous")
-    _expect(residual, "residual", (T, I), X.dtype)
+    ldr = 0
+    if bias is not None:
+        _vector(bias, "bias", I, dtype)
+    if residual is not None:
+        ldr = _rows_of(residual, "residual", T, I, dtype)
     if Y is None:
-        Y = _empty((T, I), None, X)
-    _expect(Y, "Y", (T, I), X.dtype)
+        Y, ldy = _empty((T, I), None, X), I
+    else:
+        ldy = _rows_of(Y, "Y", T, I, dtype)
     if want_ckpt or ckpt is not None:
         ckpt = _ckpt_buffer(ckpt, T, I, X)
     _check("bimask_sparse_linear_fwd",
-           lib().bimask_sparse_linear_fwd(_ptr(X), T, ldx, _ptr(Wf_values), _ptr(Wf_index), I, J, _dtype_code(X), N, M, _ptr(bias), act,
-                                          _ptr(residual), 0 if residual is None else _pitch(residual), _ptr(Y), _pitch(Y), _ptr(ckpt),
-                                          _nbytes(ckpt), _stream()))
+           lib().bimask_sparse_linear_fwd(X.data_ptr(), T, ldx, Wf_values.data_ptr(), _ptr(Wf_index), I, J, code, N, M, _ptr(bias), act,
+                                          _ptr(residual), ldr, Y.data_ptr(), ldy, _ptr(ckpt), 0 if ckpt is None else ckpt.numel(), _stream()))
     return Y, ckpt
 
 
 def bimask_act_bwd(dY, ckpt, act: int, dZ=None, dbias=None, want_dZ: bool = True, want_dbias: bool = True, workspace=None):
     """(dZ, dbias): dZ = dY * act'(Z) with Z from its checkpoint (None with ACT_NONE), dbias its column sums in fp32; either is None
     if not wanted.  dZ may be dY itself."""
-    import torch
     _on_current_device(dY, ckpt, dZ, dbias, workspace)
-    lddy = _pitch(dY)
     T, I = dY.shape
+    lddy, lddz, code = _pitch_of(dY, T, I), I, _dtype_code(dY)
     if ckpt is not None:
         _ckpt_buffer(ckpt, T, I, ckpt)
-    if dZ is None and want_dZ:
+    if dZ is not None:
+        lddz = _rows_of(dZ, "dZ", T, I, dY.dtype)
+    elif want_dZ:
         dZ = _empty((T, I), None, dY)
-    _expect(dZ, "dZ", (T, I), dY.dtype)
-    if dbias is None and want_dbias:
-        dbias = _empty((I,), torch.float32, dY)
-    _expect(dbias, "dbias", (I,), torch.float32)
-    if dbias is not None:
-        if not dbias.is_contiguous():
-            raise ValueError("dbias must be contiguous")
-        workspace = _workspace(workspace, workspace_bytes(WS_ACT_BWD, I, 0, T, 0, _dtype_code(dY), 0, 0), dY)
+    if dbias is not None or want_dbias:
+        if dbias is None:
+            dbias = _empty((I,), _torch.float32, dY)
+        else:
+            _vector(dbias, "dbias", I, _torch.float32)
+        workspace = _workspace(workspace, workspace_bytes(WS_ACT_BWD, I, 0, T, 0, code, 0, 0), dY)
     _check("bimask_act_bwd",
-           lib().bimask_act_bwd(_ptr(dY), T, lddy, _ptr(ckpt), _nbytes(ckpt), I, _dtype_code(dY), act, _ptr(dZ),
-                                0 if dZ is None else _pitch(dZ), _ptr(dbias), _ptr(workspace), _nbytes(workspace), _stream()))
+           lib().bimask_act_bwd(dY.data_ptr(), T, lddy, _ptr(ckpt), 0 if ckpt is None else ckpt.numel(), I, code, act, _ptr(dZ), lddz,
+                                _ptr(dbias), _ptr(workspace), _nbytes(workspace), _stream()))
     return dZ, dbias
 
 
@@ -503,18 +517,19 @@ def bimask_weight_grad(dY, ckpt, J: int, dW=None, dw_dtype=None, accumulate: boo
     """dW = dY^T X (I x J, dense) with X (T x J) from its checkpoint; in `dw_dtype` (that of dY if neither it nor dW says otherwise);
     accumulate: added to what dW holds."""
     _on_current_device(dY, ckpt, dW, workspace)
-    lddy = _pitch(dY)
     T, I = dY.shape
+    lddy, lddw, code = _pitch_of(dY, T, I), J, _dtype_code(dY)
     _ckpt_buffer(ckpt, T, J, ckpt)
     if dW is None:
         if accumulate:
             raise ValueError("accumulate needs a dW to add to")
         dW = _empty((I, J), dw_dtype, dY)
-    _expect(dW, "dW", (I, J), dw_dtype or dW.dtype)
-    workspace = _workspace(workspace, workspace_bytes(WS_WEIGHT_GRAD, I, J, T, 0, _dtype_code(dY), 0, 0), dY)
+    else:
+        lddw = _rows_of(dW, "dW", I, J, dw_dtype or dW.dtype)
+    workspace = _workspace(workspace, workspace_bytes(WS_WEIGHT_GRAD, I, J, T, 0, code, 0, 0), dY)
     _check("bimask_weight_grad",
-           lib().bimask_weight_grad(_ptr(dY), T, lddy, _ptr(ckpt), _nbytes(ckpt), I, J, _dtype_code(dY), _ptr(dW), _pitch(dW),
-                                    _dtype_code(dW), int(bool(accumulate)), _ptr(workspace), _nbytes(workspace), _stream()))
+           lib().bimask_weight_grad(dY.data_ptr(), T, lddy, ckpt.data_ptr(), ckpt.numel(), I, J, code, dW.data_ptr(), lddw, _dtype_code(dW),
+                                    1 if accumulate else 0, _ptr(workspace), _nbytes(workspace), _stream()))
     return dW
 
 
