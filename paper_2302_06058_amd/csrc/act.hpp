@@ -123,19 +123,20 @@ __device__ __forceinline__ float ckpt_scale(int byte) {
 // n values of a block -> their codes, four a word, first in the low byte.  v * 2^-e is exact, so adding 1.5 * 2^23 rounds it to an
 // integer (halves to even) whose two's complement stands in the low byte of the sum.
 template <int n>
-__device__ __forceinline__ void ckpt_encode(float (&v)[n], int byte, uint32_t (&out)[n / 4]) {
+__device__ __forceinline__ void ckpt_encode(const float (&v)[n], int byte, uint32_t (&out)[n / 4]) {
     const bool bad = byte == kCkptNaN;
     const float inv = ckpt_inverse(bad ? 127 : byte);
-    if (byte == 248) {                                   // e is kept to 121: up to 128 steps
-        const float most = 127.f * ckpt_scale(248);
-#pragma unroll
-        for (int i = 0; i < n; ++i) v[i] = __builtin_fminf(__builtin_fmaxf(v[i], -most), most);
-    }
 #pragma unroll
     for (int w = 0; w < n / 4; ++w) {
         uint32_t q[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) q[i] = __builtin_bit_cast(uint32_t, __builtin_fmaf(v[4 * w + i], inv, 12582912.f));
+        if (byte == 248)                                 // e is kept to 121: up to 128 steps
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int k = static_cast<int>(q[i] - 0x4B400000u);
+                q[i] = k > 127 ? 127u : k < -127 ? static_cast<uint32_t>(-127) : q[i];
+            }
         const uint32_t lo = __builtin_amdgcn_perm(q[1], q[0], 0x0C0C0400u), hi = __builtin_amdgcn_perm(q[3], q[2], 0x0C0C0400u);
         out[w] = bad ? 0u : lo | hi << 16;
     }

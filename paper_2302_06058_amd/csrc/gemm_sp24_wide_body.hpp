@@ -123,11 +123,16 @@ gemm_sp24_wide_body(const uint16_t* A, const uint32_t* Ameta, int Adim, int K, c
     f32x16 acc[TM][TN];
     auto clear = [&]() {
 #pragma unroll
-        for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i) {
+            if constexpr (OUT::kFused) out.start(acc[i][0], lane, 64 * wt + 32 * i, Adim);
 #pragma unroll
-            for (int j = 0; j < TN; ++j)
+            for (int j = OUT::kFused ? 1 : 0; j < TN; ++j) {
+                if constexpr (OUT::kFused) acc[i][j] = acc[i][0];
+                else
 #pragma unroll
-                for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
+                    for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
+            }
+        }
     };
     clear();
     int fo[4][2];                                                        // granule of k = 32 s4 + 8 h + 64 x in the row of token l32

@@ -80,12 +80,11 @@ struct LinearOut {                                       // bf16
                         z[4 * c + e] = x[e] + __builtin_bit_cast(float, e & 1 ? b[2 * c + (e >> 1)] & 0xFFFF0000u : b[2 * c + (e >> 1)] << 16);
                 }
                 if (codes) {
-                    float v[8];
                     uint32_t most = 0, d[2];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        v[e] = (e < 4 ? in0 : in1) ? z[e] : 0.f;
-                        const uint32_t m = __builtin_bit_cast(uint32_t, v[e]) & 0x7FFFFFFFu;
+                        if (!in1) z[e] = in0 && e < 4 ? z[e] : 0.f;      // (nothing of theirs is stored)
+                        const uint32_t m = __builtin_bit_cast(uint32_t, z[e]) & 0x7FFFFFFFu;
                         most = m > most ? m : most;
                     }
                     uint32_t o = __builtin_amdgcn_mov_dpp(most, 0xB1, 0xF, 0xF, true);       // the other lane of a pair, the other pair of four
@@ -93,7 +92,7 @@ struct LinearOut {                                       // bf16
                     o = __builtin_amdgcn_mov_dpp(most, 0x4E, 0xF, 0xF, true);
                     most = o > most ? o : most;
                     const int byte = ckpt_scale_byte(most);
-                    ckpt_encode(v, byte, d);
+                    ckpt_encode(z, byte, d);
                     if (a < pitch) {
                         *reinterpret_cast<u32x2*>(codes + (t0 + t) * pitch + a) = (u32x2){d[0], d[1]};
                         if ((u & 3) == 0) scales[(t0 + t) * (pitch / 32) + a / 32] = static_cast<uint8_t>(byte);
@@ -120,8 +119,8 @@ struct LinearOut {                                       // bf16
         }
     }
 
-    // The same within one wavefront, on two accumulators (64 weight rows from a0 x 32 tokens from t0, `rows` of which exist) before they
-    // are rounded: bias, checkpoint, activation and residual.  strip: 32 rows of 136 bytes of the wavefront's own.
+    // The same within one wavefront, on two accumulators (64 weight rows from a0 x 32 tokens from t0, `rows` of which exist) that began
+    // with the bias (start), before they are rounded: checkpoint, activation and residual.  strip: 32 rows of 136 bytes of the wavefront's own.
     // `ahead`: with AHEAD this residual piece, requested before (fetch_residual), replaced by the next one's if there is one.
     typedef unsigned int Piece __attribute__((ext_vector_type(4)));
     __device__ __forceinline__ void fetch_residual(Piece (&ahead)[4], int lane, int a0, int64_t t0, int rows, int Adim) const {
@@ -130,6 +129,18 @@ struct LinearOut {                                       // bf16
         for (int it = 0; it < 4; ++it) {                 // beyond the tile: loaded from its first piece, not used
             const int r = (lane >> 3) + 8 * it, c = 8 * (lane & 7);
             ahead[it] = *reinterpret_cast<const Piece*>(R + (t0 + (r < rows ? r : 0)) * ldr + a0 + (c < Adim - a0 ? c : 0));      // Adim is a multiple of 8
+        }
+    }
+    template <class ACC>
+    __device__ __forceinline__ void start(ACC& z, int lane, int a, int Adim) const {
+        typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+        const int h = lane >> 5;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            u32x2 b = {0u, 0u};
+            if (bias && a + 8 * q + 4 * h < Adim) b = *reinterpret_cast<const u32x2*>(bias + a + 8 * q + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[4 * q + e] = __builtin_bit_cast(float, e & 1 ? b[e >> 1] & 0xFFFF0000u : b[e >> 1] << 16);
         }
     }
     template <bool AHEAD, class ACC>
@@ -151,36 +162,28 @@ struct LinearOut {                                       // bf16
             if (AHEAD && more) fetch_residual(ahead, lane, a0, t0 + 32, rows - 32, Adim);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        int byte[2] = {0, 0};
         auto half = [&](ACC& z, int i) {
             float y[16];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int a = a0 + 32 * i + 8 * q + 4 * h;
-                u32x2 b = {0u, 0u};
-                if (bias && a < Adim) b = *reinterpret_cast<const u32x2*>(bias + a);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    y[4 * q + e] = z[4 * q + e] + __builtin_bit_cast(float, e & 1 ? b[e >> 1] & 0xFFFF0000u : b[e >> 1] << 16);
-            }
+            for (int q = 0; q < 16; ++q) y[q] = z[q];
             if (codes && a0 + 32 * i < Adim) {
-                float v[16];
                 uint32_t most = 0, d[4];
+                if (a0 + 32 * i + 32 > Adim)             // uniform, the last tile: features that do not exist count as 0
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) y[q] = a0 + 32 * i + 8 * (q >> 2) + 4 * h < Adim ? y[q] : 0.f;
 #pragma unroll
                 for (int q = 0; q < 16; ++q) {
-                    v[q] = a0 + 32 * i + 8 * (q >> 2) + 4 * h < Adim ? y[q] : 0.f;
-                    const uint32_t m = __builtin_bit_cast(uint32_t, v[q]) & 0x7FFFFFFFu;
+                    const uint32_t m = __builtin_bit_cast(uint32_t, y[q]) & 0x7FFFFFFFu;
                     most = m > most ? m : most;
                 }
                 const auto both = __builtin_amdgcn_permlane32_swap(most, most, false, false);
-                const int byte = ckpt_scale_byte(both[0] > both[1] ? both[0] : both[1]);
-                ckpt_encode(v, byte, d);
+                byte[i] = ckpt_scale_byte(both[0] > both[1] ? both[0] : both[1]);
+                ckpt_encode(y, byte[i], d);
                 const auto lo = __builtin_amdgcn_permlane32_swap(d[0], d[2], false, false);
                 const auto hi = __builtin_amdgcn_permlane32_swap(d[1], d[3], false, false);
-                if (l32 < rows) {
-                    const int64_t pitch = ckpt_pitch(Adim);
-                    *reinterpret_cast<u32x4*>(codes + t * pitch + a0 + 32 * i + 16 * h) = (u32x4){lo[0], lo[1], hi[0], hi[1]};
-                    if (h == 0) scales[t * (pitch / 32) + a0 / 32 + i] = static_cast<uint8_t>(byte);
-                }
+                if (l32 < rows)
+                    *reinterpret_cast<u32x4*>(codes + t * ckpt_pitch(Adim) + a0 + 32 * i + 16 * h) = (u32x4){lo[0], lo[1], hi[0], hi[1]};
             }
             apply_act<true>(y, act);
             if (R) {
@@ -205,6 +208,12 @@ struct LinearOut {                                       // bf16
         };
         half(z0, 0);
         half(z1, 1);
+        if (codes && h == 0 && l32 < rows) {             // both blocks' scale bytes at once
+            typedef uint16_t u16_any __attribute__((aligned(1)));
+            uint8_t* p = scales + t * ckpt_blocks(Adim) + a0 / 32;
+            if (a0 + 32 < Adim) *reinterpret_cast<u16_any*>(p) = static_cast<uint16_t>(byte[0] | byte[1] << 8);
+            else *p = static_cast<uint8_t>(byte[0]);
+        }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 };
