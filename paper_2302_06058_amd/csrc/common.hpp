@@ -269,7 +269,7 @@ int launch_linear(const void* A, const uint32_t* meta, int64_t Adim, int64_t K, 
 
 // dW = dY^T X~ from X's checkpoint (weight_grad.hip)
 struct WeightGradPlan {
-    enum Tile { k128x128, k256x256, k64x256, k256x64 } tile;      // output tile (bf16)
+    enum Tile { k128x128, k256x256, k64x192, k64x256, k256x64, k64x64 } tile;      // output tile (the last: fp32)
     int64_t rows;        // tokens of a piece
     int64_t pieces;
     size_t ws_bytes;     // sums of the pieces

@@ -50,6 +50,10 @@ __device__ __forceinline__ void put(int mode, void* out, int64_t at, float v) {
     else put<kAddBF16>(out, at, v);
 }
 
+// LDS bytes: three stages, later the wavefronts' output strips
+template <int BM, int BN, int WM, int WN>
+constexpr int kGradLds = 3 * kStageT * (BM + BN) * 2 > WM * WN * 32 * (BN / WN + 4) * 4 ? 3 * kStageT * (BM + BN) * 2 : WM * WN * 32 * (BN / WN + 4) * 4;
+
 // BM x BN output tile on WM x WN wavefronts.  WHOLE: I >= 8 and 32 rows of either operand span less than 2^31 bytes.  Rows of dY
 // may start on any element (the 16-byte loads need no more).  Where I is no multiple of 8, the piece that would run over the row's
 // end is the row's last 8 features instead: its first `over` rows of the output come twice, the others `over` places late.
@@ -82,10 +86,10 @@ k_weight_grad(const uint16_t* __restrict__ dY, int64_t T, int64_t lddy, const ui
     const int64_t pitch = ckpt_pitch(J), blocks = ckpt_blocks(J);
     const int stages = static_cast<int>(t_begin < t_end ? ceil_div(t_end - t_begin, kStageT) : 0);
 
-    const bool has_b = kStageT * BN / 16 >= NT || tid < kStageT * BN / 16;        // 64 columns: codes for half of the threads
+    auto has_b = [&](int p) { return kStageT * BN / 16 >= NT * (p + 1) || tid + NT * p < kStageT * BN / 16; };      // 64 and 192 columns: pieces for some of the threads
 
-    auto swz_a = [](int row) { return BM >= 128 ? row & 3 : (row >> 1) & 1; };
-    auto swz_b = [](int row) { return BN >= 128 ? row & 3 : (row >> 1) & 1; };
+    auto swz_a = [](int row) { return BM % 128 == 0 ? row & 3 : (row >> 1) & 1; };
+    auto swz_b = [](int row) { return BN % 128 == 0 ? row & 3 : (row >> 1) & 1; };
 
     u32x4 ra[SETS][PA], rb[SETS][PB];
     int rs[SETS][PB];
@@ -99,9 +103,9 @@ k_weight_grad(const uint16_t* __restrict__ dY, int64_t T, int64_t lddy, const ui
 #pragma unroll
         for (int p = 0; p < PB; ++p) {
             const int q = tid + NT * p, row = q / (BN / 16), u = q % (BN / 16);
-            const int64_t j = j0 + 16 * u < pitch && has_b ? j0 + 16 * u : 0;
-            off_b[p] = static_cast<uint32_t>((has_b ? row : 0) * pitch + j);
-            off_s[p] = static_cast<uint32_t>((has_b ? row : 0) * blocks + j / 32);
+            const int64_t j = j0 + 16 * u < pitch && has_b(p) ? j0 + 16 * u : 0;
+            off_b[p] = static_cast<uint32_t>((has_b(p) ? row : 0) * pitch + j);
+            off_s[p] = static_cast<uint32_t>((has_b(p) ? row : 0) * blocks + j / 32);
         }
     }
     // WHOLE: the rows of the next stage to request, as buffers that end with the piece's last row
@@ -141,7 +145,7 @@ k_weight_grad(const uint16_t* __restrict__ dY, int64_t T, int64_t lddy, const ui
             for (int p = 0; p < PB; ++p) {
                 const int q = tid + NT * p, row = q / (BN / 16), u = q % (BN / 16);
                 const int64_t t = t0 + row, j = j0 + 16 * u;
-                const bool in = has_b && t < t_end && j < pitch;
+                const bool in = has_b(p) && t < t_end && j < pitch;
                 const u32x4 v = *reinterpret_cast<const u32x4*>(codes + (in ? t * pitch + j : 0));
                 rb[set][p] = in ? v : (u32x4){0u, 0u, 0u, 0u};
                 rs[set][p] = in ? scales[t * blocks + j / 32] : 0;
@@ -169,7 +173,7 @@ k_weight_grad(const uint16_t* __restrict__ dY, int64_t T, int64_t lddy, const ui
                     const uint32_t four = rb[set][p][2 * x + (d >> 1)];
                     v[d] = pack_bf16(ckpt_value(four, 2 * (d & 1), scale), ckpt_value(four, 2 * (d & 1) + 1, scale));
                 }
-                if (has_b) *reinterpret_cast<u32x4*>(dst + 16 * x) = v;
+                if (has_b(p)) *reinterpret_cast<u32x4*>(dst + 16 * x) = v;
             }
         }
     };
@@ -268,7 +272,7 @@ k_weight_grad(const uint16_t* __restrict__ dY, int64_t T, int64_t lddy, const ui
     void* dst = split ? static_cast<void*>(part + static_cast<int64_t>(piece) * I * J) : out;
     const int64_t ld = split ? J : ldo;
     constexpr int COLS = 32 * TN, PITCH = COLS + 4;
-    static_assert(WM * WN * 32 * PITCH * 4 <= 3 * (SA + SB) && COLS % 64 == 0, "strips fit the stage buffers");
+    static_assert(COLS == BN / WN && WM * WN * 32 * PITCH * 4 <= kGradLds<BM, BN, WM, WN>, "strips fit");
     float* strip = reinterpret_cast<float*>(smem) + wave * (32 * PITCH);
     const int64_t col0 = j0 + wn * COLS + lane;
     __syncthreads();                                     // every wavefront is done with the stage buffers
@@ -286,7 +290,7 @@ k_weight_grad(const uint16_t* __restrict__ dY, int64_t T, int64_t lddy, const ui
             for (int r = 0; r < n_rows; ++r)
 #pragma unroll
                 for (int c = 0; c < COLS; c += 64)
-                    if (col0 + c < J) put<decltype(mode_c)::value>(dst, (row0 + r) * ld + col0 + c, strip[(r + (r >= late ? over : 0)) * PITCH + c + lane]);
+                    if (col0 + c < J && c + lane < COLS) put<decltype(mode_c)::value>(dst, (row0 + r) * ld + col0 + c, strip[(r + (r >= late ? over : 0)) * PITCH + c + lane]);
         };
         if (split || mode == kOutF32) write(std::integral_constant<int, kOutF32>{});
         else if (mode == kOutBF16) write(std::integral_constant<int, kOutBF16>{});
@@ -362,7 +366,37 @@ k_weight_grad_f32(const float* __restrict__ dY, int64_t T, int64_t lddy, const u
         }
 }
 
-// 64 elements x 4 ranges of pieces per workgroup, added in a fixed order on both levels
+// Sums of the pieces, added in piece order.  Few pieces: four consecutive elements a thread.  Many (a small matrix): 64 elements x 4
+// ranges of pieces per workgroup, so that the chain of additions is a quarter as long.
+constexpr int kFewPieces = 12;
+
+__global__ void __launch_bounds__(kThreads)
+k_sum_few_pieces(const float* __restrict__ part, int pieces, int64_t I, int64_t J, void* out, int64_t ldo, int mode) {
+    typedef f32x4 f32x4_any __attribute__((aligned(4)));
+    const int64_t total = I * J;
+    for (int64_t e = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) * 4; e < total; e += static_cast<int64_t>(gridDim.x) * kThreads * 4) {
+        const int n = static_cast<int>(total - e < 4 ? total - e : 4);
+        const int64_t from = e + 4 <= total ? e : total >= 4 ? total - 4 : 0;        // the last elements: four that exist
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+        if (total >= 4) {
+#pragma unroll 4
+            for (int k = 0; k < pieces; ++k) s += __builtin_nontemporal_load(reinterpret_cast<const f32x4_any*>(part + k * total + from));
+        } else {
+            for (int k = 0; k < pieces; ++k)
+                for (int x = 0; x < n; ++x) s[x] += part[k * total + x];
+        }
+        int64_t i = e / J, j = e - i * J;
+        const int skip = static_cast<int>(e - from);
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            if (x < n) {
+                const float v = skip + x == 0 ? s[0] : skip + x == 1 ? s[1] : skip + x == 2 ? s[2] : s[3];
+                put(mode, out, i * ldo + j, v);
+                if (++j == J) { j = 0; ++i; }
+            }
+    }
+}
+
 __global__ void __launch_bounds__(kThreads)
 k_sum_pieces(const float* __restrict__ part, int pieces, int64_t I, int64_t J, void* out, int64_t ldo, int mode) {
     __shared__ float sums[4][64];
@@ -392,7 +426,7 @@ struct Operands {
 
 template <int BM, int BN, int WM, int WN, int SETS, bool WHOLE>
 int run(const Operands& o, const WeightGradPlan& p) {
-    constexpr int lds = 3 * kStageT * (BM + BN) * 2;
+    constexpr int lds = kGradLds<BM, BN, WM, WN>;
     auto kern = k_weight_grad<BM, BN, WM, WN, SETS, WHOLE>;
     if (lds > 48 * 1024) {
         static DeviceMemo attr_set;
@@ -413,18 +447,45 @@ int run(const Operands& o, const WeightGradPlan& p) {
 
 }  // namespace
 
+// Tile and pieces.  A 256 x 256 tile moves half the LDS bytes of four 128 x 128 ones per product (2048 x 2048 with 4096 tokens 56 us
+// in 4 pieces of the 64 tiles, 61 with 256 tiles of 128 x 128; 1024 x 4096 with 8192 81 / 96), as long as tiles and pieces fill the 256
+// CUs once without much padding and a piece has the stages that pay for its sums (1024 x 1024 with 4096 34 / 30, 3000 x 1000 with 2000
+// 37 / 31).  Narrow matrices: tiles as narrow.  The others: two workgroups per CU are there at once, so at most 512, pieces of 16
+// stages or more, and none where the tiles alone fill half of the CUs (3000 x 1000 with 2000 tokens 31 us, in two pieces 35).
 WeightGradPlan plan_weight_grad(int64_t T, int64_t I, int64_t J, int dtype) {
     WeightGradPlan p;
-    const bool f32 = dtype == BIMASK_F32;
-    p.tile = ceil_div(I, 256) * ceil_div(J, 256) >= 192 ? WeightGradPlan::k256x256
-           : I <= 64 && J > 64 ? WeightGradPlan::k64x256 : J <= 64 && I > 64 ? WeightGradPlan::k256x64 : WeightGradPlan::k128x128;
-    const bool big = !f32 && p.tile == WeightGradPlan::k256x256;
-    const int64_t bm = f32 ? kTileF32 : p.tile == WeightGradPlan::k64x256 ? 64 : p.tile == WeightGradPlan::k256x64 ? 256 : 128;
-    const int64_t bn = f32 ? kTileF32 : p.tile == WeightGradPlan::k64x256 ? 256 : p.tile == WeightGradPlan::k256x64 ? 64 : 128;
-    const int64_t tiles = ceil_div(I, bm) * ceil_div(J, bn), stage = f32 ? kStageF32 : kStageT, stages = ceil_div(T, stage);
-    // pieces: at most 512 workgroups (two per CU are there at once; a few more would run after them), none with fewer than 8 stages
-    int64_t pieces = big || tiles > 256 ? 1 : 512 / tiles;
-    const int64_t most = stages / 8 > 1 ? stages / 8 : 1;
+    int64_t bm, bn, stage = kStageT, pieces;
+    if (dtype == BIMASK_F32) {
+        p.tile = WeightGradPlan::k64x64;
+        bm = bn = kTileF32;
+        stage = kStageF32;
+    } else if (I <= 64 && J > 64) {
+        p.tile = round_up(J, 192) < round_up(J, 256) ? WeightGradPlan::k64x192 : WeightGradPlan::k64x256;
+        bm = 64;
+        bn = p.tile == WeightGradPlan::k64x192 ? 192 : 256;
+    } else if (J <= 64 && I > 64) {
+        p.tile = WeightGradPlan::k256x64;
+        bm = 256;
+        bn = 64;
+    } else {
+        p.tile = WeightGradPlan::k128x128;
+        bm = bn = 128;
+    }
+    const int64_t stages = ceil_div(T, stage), tiles = ceil_div(I, bm) * ceil_div(J, bn), large = ceil_div(I, 256) * ceil_div(J, 256);
+    pieces = tiles >= 128 ? 1 : 512 / tiles;
+    int64_t least = p.tile == WeightGradPlan::k128x128 ? 16 : 8;
+    if (p.tile == WeightGradPlan::k128x128) {
+        const int64_t n = large >= 256 ? 1 : 256 / large;
+        const double filled = static_cast<double>(I) * static_cast<double>(J) / (static_cast<double>(large) * 65536) *
+                              static_cast<double>(large * n) / static_cast<double>(round_up(large * n, 256));
+        if (filled >= 0.75 && (n == 1 || stages / n >= 24)) {
+            p.tile = WeightGradPlan::k256x256;
+            pieces = n;
+        }
+    } else if (p.tile == WeightGradPlan::k64x64) {
+        pieces = tiles > 256 ? 1 : 512 / tiles;
+    }
+    const int64_t most = stages / least > 1 ? stages / least : 1;
     pieces = pieces < most ? pieces : most;
     p.rows = ceil_div(stages, pieces) * stage;
     p.pieces = ceil_div(T, p.rows);
@@ -448,14 +509,16 @@ int launch_weight_grad(const void* dY, int64_t T, int64_t lddy, const uint8_t* c
     } else {
         if (I < 8 || lddy >= (1 << 24) || J >= (1 << 25) || T >= (1ll << 31)) rc = run<128, 128, 2, 2, 2, false>(o, p);
         else if (p.tile == WeightGradPlan::k256x256) rc = run<256, 256, 2, 4, 2, true>(o, p);
+        else if (p.tile == WeightGradPlan::k64x192) rc = run<64, 192, 2, 2, 4, true>(o, p);
         else if (p.tile == WeightGradPlan::k64x256) rc = run<64, 256, 1, 4, 4, true>(o, p);
         else if (p.tile == WeightGradPlan::k256x64) rc = run<256, 64, 4, 1, 4, true>(o, p);
         else rc = run<128, 128, 2, 2, 4, true>(o, p);
     }
     if (rc || p.pieces == 1) return rc;
-    const int64_t n = ceil_div(I * J, 64);
-    hipLaunchKernelGGL(k_sum_pieces, dim3(static_cast<unsigned>(n < (1 << 20) ? n : 1 << 20)), dim3(kThreads), 0, s, ws, static_cast<int>(p.pieces), I, J,
-                       dW, lddw, mode);
+    const bool few = p.pieces <= kFewPieces;
+    const int64_t n = ceil_div(I * J, few ? 4 * kThreads : 64);
+    hipLaunchKernelGGL(few ? k_sum_few_pieces : k_sum_pieces, dim3(static_cast<unsigned>(n < (1 << 20) ? n : 1 << 20)), dim3(kThreads), 0, s, ws,
+                       static_cast<int>(p.pieces), I, J, dW, lddw, mode);
     return check_launch();
 }
 
