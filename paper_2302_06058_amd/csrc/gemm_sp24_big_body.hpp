@@ -258,7 +258,7 @@ gemm_sp24_big_body(const uint16_t* A, const uint32_t* Ameta, int64_t Adim, int n
             if constexpr (OUT::kFused) {
                 const int ta = pos / nt, tt = pos - ta * nt;
                 __syncthreads();                         // the previous tile's sums have been read
-                out.template finish<kBigRows, BN, 32 * TM, BN, TM, TN, NT, 1, 4>(acc, sOut, 0, wave, 0, lane, static_cast<int64_t>(ta) * kBigRows,
+                out.template finish<kBigRows, BN, 32 * TM, BN, TM, TN, NT, 1, 4, true>(acc, sOut, 0, wave, 0, lane, static_cast<int64_t>(ta) * kBigRows,
                                                                                  static_cast<int64_t>(t_begin + tt) * kBigTokens, Adim, T, C, ldc, true);
 #pragma unroll
                 for (int i = 0; i < TM; ++i)

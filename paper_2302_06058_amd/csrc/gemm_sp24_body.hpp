@@ -254,7 +254,7 @@ gemm_sp24_body(const uint16_t* A, const uint32_t* Ameta, int64_t Adim, int64_t K
     __syncthreads();                                     // every wavefront is done with the last stage
     if constexpr (OUT::kFused) {
         constexpr int PASSES = (4 * KG * BN * BM + S::kTotal - 1) / S::kTotal;
-        out.template finish<BM, BN, WM, WN, TM, TN, NT * KG, KG, PASSES>(acc, smem, kg, wm, wn, lane, a0, t0, Adim, T, C, ldc, vecC);
+        out.template finish<BM, BN, WM, WN, TM, TN, NT * KG, KG, PASSES, false>(acc, smem, kg, wm, wn, lane, a0, t0, Adim, T, C, ldc, vecC);
         return;
     }
     if constexpr (KG > 1) {

@@ -21,21 +21,51 @@ struct LinearOut {                                       // bf16
     // every thread then takes 8 consecutive features of a token at a time: residual and output move as whole row segments, a block of
     // the checkpoint is four neighbouring lanes, the groups' shares are added in group order.
     // Adim is a multiple of 4, so a piece's halves are inside or outside; sums beyond it may be NaN and count as 0 in the checkpoint.
-    template <int BM, int BN, int WM, int WN, int TM, int TN, int NT, int KG, int PASSES, class ACC>
+    // TIGHT: the state of a persistent loop leaves few registers: nothing is requested ahead, addresses are made when needed.
+    template <int BM, int BN, int WM, int WN, int TM, int TN, int NT, int KG, int PASSES, bool TIGHT, class ACC>
     __device__ __forceinline__ void finish(ACC (&acc)[TM][TN], uint8_t* smem, int kg, int wm, int wn, int lane, int64_t a0, int64_t t0,
                                            int64_t Adim, int64_t T, uint16_t* C, int64_t ldc, bool vecC) const {
         typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
         typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
         typedef float f32x4 __attribute__((ext_vector_type(4)));
-        constexpr int ROWS = BM / PASSES, UPR = ROWS / 8;            // features of a token in a pass, pieces of 8
-        static_assert(ROWS % WM == 0, "a pass takes whole wavefronts");
+        constexpr int ROWS = BM / PASSES, UPR = ROWS / 8, STEP = NT / UPR;        // pieces of 8 features; tokens from one piece of a thread to its next
+        static_assert(ROWS % WM == 0 && NT % UPR == 0, "a pass takes whole wavefronts, a thread keeps its features");
         int tid = threadIdx.x;
         asm volatile("" : "+v"(lane), "+v"(tid));        // (what depends on them is not kept across the caller's loop)
         f32x4* sums = reinterpret_cast<f32x4*>(smem);
         auto chunk = [](int g, int t, int c) { return (g * BN + t) * (ROWS / 4) + (c ^ (t & (ROWS < 64 ? 7 : 15))); };
         const int64_t pitch = ckpt_pitch(Adim);
+        const int n_tok = static_cast<int>(T - t0 < BN ? T - t0 : BN), u = tid % UPR;
 #pragma unroll 1
         for (int pass = 0; pass < PASSES; ++pass) {
+            const int64_t a = a0 + pass * ROWS + 8 * u;
+            const bool in0 = a < Adim, in1 = a + 4 < Adim;
+            int t = tid / UPR;
+            const uint16_t* src = R + (t0 + t) * ldr + a;
+            auto fetch = [&](u32x4& r, const uint16_t* src) {      // the residual of a piece
+                if (vecR && in1) {
+                    r = *reinterpret_cast<const u32x4*>(src);
+                } else if (in0) {                        // 4-byte pieces (pointer and pitch are 4-byte aligned, Adim even)
+#pragma unroll
+                    for (int d = 0; d < 4; ++d)
+                        if (d < 2 || in1) r[d] = *reinterpret_cast<const uint32_t*>(src + 2 * d);
+                }
+            };
+            u32x4 ahead = {0u, 0u, 0u, 0u};              // requested before the sums are exchanged, and one piece ahead from then on
+            if (!TIGHT && R && t < n_tok) fetch(ahead, src);
+            auto fetch_bias = [&]() {
+                u32x4 b = {0u, 0u, 0u, 0u};
+                if (bias && in0) {
+                    const u32x2 x = *reinterpret_cast<const u32x2*>(bias + a);
+                    b.x = x.x; b.y = x.y;
+                    if (in1) {
+                        const u32x2 w = *reinterpret_cast<const u32x2*>(bias + a + 4);
+                        b.z = w.x; b.w = w.y;
+                    }
+                }
+                return b;
+            };
+            const u32x4 b_kept = TIGHT ? (u32x4){0u, 0u, 0u, 0u} : fetch_bias();
             if (pass > 0) __syncthreads();               // the previous pass has been read
             if (PASSES == 1 || wm * WM / ROWS == pass)
 #pragma unroll
@@ -47,27 +77,23 @@ struct LinearOut {                                       // bf16
                             sums[chunk(kg, wn * WN + 32 * j + (lane & 31), (wm * WM % ROWS + 32 * i) / 4 + 2 * q + (lane >> 5))] =
                                 (f32x4){acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
             __syncthreads();
-            const int n_tok = static_cast<int>(T - t0 < BN ? T - t0 : BN);
+            uint16_t* dst = C + (t0 + t) * ldc + a;
+            uint8_t* dst_code = codes + (t0 + t) * pitch + a;
+            uint8_t* dst_scale = scales + (t0 + t) * (pitch / 32) + a / 32;
 #pragma unroll 1
-            for (int q = tid; q < n_tok * UPR; q += NT) {
-                const int t = q / UPR, u = q % UPR;
-                const int64_t a = a0 + pass * ROWS + 8 * u;
-                const bool in0 = a < Adim, in1 = a + 4 < Adim;
-                u32x4 r = {0u, 0u, 0u, 0u};
-                if (R && in0) {
-                    const uint16_t* src = R + (t0 + t) * ldr + a;
-                    if (vecR && in1) {
-                        r = *reinterpret_cast<const u32x4*>(src);
-                    } else {                             // 4-byte pieces (pointer and pitch are 4-byte aligned, Adim even)
-#pragma unroll
-                        for (int d = 0; d < 4; ++d)
-                            if (d < 2 || in1) r[d] = *reinterpret_cast<const uint32_t*>(src + 2 * d);
-                    }
-                }
-                u32x4 b = {0u, 0u, 0u, 0u};
-                if (bias) {
-                    if (in0) *reinterpret_cast<u32x2*>(&b) = *reinterpret_cast<const u32x2*>(bias + a);
-                    if (in1) reinterpret_cast<u32x2*>(&b)[1] = *reinterpret_cast<const u32x2*>(bias + a + 4);
+            for (; t < n_tok; t += STEP) {
+                u32x4 r = ahead, b = b_kept;
+                if constexpr (TIGHT) {
+                    int tt = t;
+                    asm volatile("" : "+v"(tt));         // (or the addresses would be kept and stepped)
+                    if (R) fetch(r, R + (t0 + tt) * ldr + a);
+                    b = fetch_bias();
+                    dst = C + (t0 + tt) * ldc + a;
+                    dst_code = codes + (t0 + tt) * pitch + a;
+                    dst_scale = scales + (t0 + tt) * (pitch / 32) + a / 32;
+                } else if (R && t + STEP < n_tok) {
+                    src += STEP * ldr;
+                    fetch(ahead, src);
                 }
                 float z[8];
 #pragma unroll
@@ -81,9 +107,11 @@ struct LinearOut {                                       // bf16
                 }
                 if (codes) {
                     uint32_t most = 0, d[2];
+                    if (!in1)                            // (nothing of theirs is stored)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) z[e] = in0 && e < 4 ? z[e] : 0.f;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        if (!in1) z[e] = in0 && e < 4 ? z[e] : 0.f;      // (nothing of theirs is stored)
                         const uint32_t m = __builtin_bit_cast(uint32_t, z[e]) & 0x7FFFFFFFu;
                         most = m > most ? m : most;
                     }
@@ -94,9 +122,11 @@ struct LinearOut {                                       // bf16
                     const int byte = ckpt_scale_byte(most);
                     ckpt_encode(z, byte, d);
                     if (a < pitch) {
-                        *reinterpret_cast<u32x2*>(codes + (t0 + t) * pitch + a) = (u32x2){d[0], d[1]};
-                        if ((u & 3) == 0) scales[(t0 + t) * (pitch / 32) + a / 32] = static_cast<uint8_t>(byte);
+                        *reinterpret_cast<u32x2*>(dst_code) = (u32x2){d[0], d[1]};
+                        if ((u & 3) == 0) *dst_scale = static_cast<uint8_t>(byte);
                     }
+                    dst_code += STEP * pitch;
+                    dst_scale += STEP * (pitch / 32);
                 }
                 apply_act<true>(z, act);
                 u32x4 y;
@@ -105,16 +135,14 @@ struct LinearOut {                                       // bf16
                     const float lo = __builtin_bit_cast(float, r[d] << 16), hi = __builtin_bit_cast(float, r[d] & 0xFFFF0000u);
                     y[d] = R ? pack_bf16(z[2 * d] + lo, z[2 * d + 1] + hi) : pack_bf16(z[2 * d], z[2 * d + 1]);
                 }
-                if (in0) {
-                    uint16_t* dst = C + (t0 + t) * ldc + a;
-                    if (vecC && in1) {
-                        __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(dst));
-                    } else {
+                if (vecC && in1) {
+                    __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(dst));
+                } else if (in0) {
 #pragma unroll
-                        for (int d = 0; d < 4; ++d)
-                            if (d < 2 || in1) reinterpret_cast<uint32_t*>(dst)[d] = y[d];
-                    }
+                    for (int d = 0; d < 4; ++d)
+                        if (d < 2 || in1) reinterpret_cast<uint32_t*>(dst)[d] = y[d];
                 }
+                dst += STEP * ldc;
             }
         }
     }
