@@ -32,10 +32,10 @@ def dev(a, dtype):
 
 
 def strided(a, dtype, pad, first=0, fill=0.0):
-    """`a` as a view into a wider buffer, `first` elements in; returns (view, buffer)."""
+    """`a` as a view into a wider buffer, `first` elements in and with room for three more rows; returns (view, buffer)."""
     import torch
     T, C = a.shape
-    buf = torch.full((first + T * (C + pad),), fill, dtype=tdt(dtype), device="cuda")
+    buf = torch.full((first + (T + 3) * (C + pad),), fill, dtype=tdt(dtype), device="cuda")
     v = buf[first:first + T * (C + pad)].view(T, C + pad)[:, :C]
     v.copy_(dev(a, dtype))
     return v, buf
@@ -77,7 +77,7 @@ def test_checkpoint_is_the_rule_bit_by_bit(T, C, dtype, pad, first):
     bm.bimask_checkpoint_load(buf[:n], T, C, X=out)
     assert (from_dev_f64(out, dtype) == ref.load(codes, scales, C)).all()
     out.fill_(5.0)
-    assert (whole == 5.0).all(), "written beside the rows"
+    assert (whole == 5.0).all(), "written beside or behind the rows"
     assert torch.equal(bm.bimask_checkpoint_load(buf[:n], T, C, tdt(dtype)), bm.bimask_checkpoint_load(buf[:n], T, C, torch.float32).to(tdt(dtype)))
 
 
@@ -168,7 +168,7 @@ def test_linear_sums_are_exact_with_bias_residual_and_checkpoint(I, J, T, N, M, 
     live = np.abs(codes.reshape(T, -1, 32)).max(-1) > 0
     assert (gc == codes).all() and (gs == scales)[live].all()
     Y.fill_(99.0)
-    assert (whole == 99.0).all(), "written beside the rows"
+    assert (whole == 99.0).all(), "written beside or behind the rows"
     # without anything, and the relu: exact as well; in place on the residual
     assert (from_dev_f64(bm.bimask_sparse_linear_fwd(X, v, idx, I, J, N, M)[0], dtype) == x @ Wm.T).all()
     bm.bimask_sparse_linear_fwd(X, v, idx, I, J, N, M, bias=dev(bias[None], dtype)[0], act=bm.ACT_RELU, residual=R, Y=R)
@@ -270,7 +270,7 @@ def test_act_bwd(T, I, a, dtype):
         bm.bimask_act_bwd(D, ck, bm.ACTS[a], dZ=D, want_dbias=False)                    # in place
         assert torch.equal(D, dZ)
         dZ.fill_(9.0)
-        assert (whole == 9.0).all(), "written beside the rows"
+        assert (whole == 9.0).all(), "written beside or behind the rows"
 
 
 @pytest.mark.parametrize("a", ref.ACTS[1:])
@@ -322,7 +322,7 @@ def test_weight_grad_sums_are_exact(I, J, T, dtype, dw, pad):
     assert (from_dev_f64(dW, dw) == rounded(want + old, dw)).all()
     assert torch.equal(bm.bimask_weight_grad(D, ck, J, dw_dtype=tdt(dw)), dev(want, dw))
     dW.fill_(7.0)
-    assert (whole == 7.0).all(), "written beside the rows"
+    assert (whole == 7.0).all(), "written beside or behind the rows"
 
 
 @pytest.mark.parametrize("I,J,T,dtype", [(64, 576, 5000, BF), (300, 200, 9000, BF), (200, 96, 3000, F32), (4096, 3336, 2000, BF)])
@@ -482,3 +482,97 @@ def test_single_rows_and_columns_of_other_layouts():
     assert (from_dev_f64(bm.bimask_sparse_linear_fwd(X[::2], v, idx, 32, 64, 2, 4)[0], BF) == x[::2] @ Wm.T).all()
     col = dev(rng.integers(-3, 4, (9, 4)).astype(float), F32)[:, 1:2]
     assert torch.equal(bm.bimask_checkpoint_load(bm.bimask_checkpoint_store(col), 9, 1, torch.float32), col)
+
+
+def test_outputs_stay_within_checkpoint_and_workspace():
+    """Bytes behind a checkpoint that the product writes, and behind workspaces, stay as they were."""
+    import torch
+    rng = np.random.default_rng(7)
+    for I, J, T, dtype in ((36, 64, 5, BF), (100, 1100, 37, BF), (1008, 136, 6200, BF), (40, 64, 5, F32)):
+        W, _ = masked_integers(rng, I, J, 2, 4)
+        v, idx = operand(W, 2, 4, dtype)
+        n = bm.checkpoint_bytes(T, I)
+        buf = torch.full((n + 256,), 99, dtype=torch.uint8, device="cuda")
+        X = dev(few_ones(rng, T, J), dtype)
+        Y, ck = bm.bimask_sparse_linear_fwd(X, v, idx, I, J, 2, 4, ckpt=buf[:n])
+        assert ck.data_ptr() == buf.data_ptr() and (buf[n:] == 99).all()
+        assert torch.equal(ck, bm.bimask_sparse_linear_fwd(X, v, idx, I, J, 2, 4, want_ckpt=True)[1])
+    for I, J, T in ((64, 576, 5000), (300, 200, 9000), (512, 512, 49999)):
+        for kind, call in ((bm.WS_ACT_BWD, lambda ws: bm.bimask_act_bwd(dY, None, bm.ACT_NONE, want_dZ=False, workspace=ws)[1]), (bm.WS_WEIGHT_GRAD, lambda ws: bm.bimask_weight_grad(dY, ck, J, workspace=ws))):
+            dY = dev(rng.integers(-2, 3, (T, I)).astype(float), BF)
+            ck = bm.bimask_checkpoint_store(dev(rng.integers(-2, 3, (T, J)).astype(float), BF))
+            need = bm.workspace_bytes(kind, I, J, T, 0, bm.BF16, 0, 0)
+            assert need > 0
+            buf = torch.full((need + 256,), 99, dtype=torch.uint8, device="cuda")
+            assert torch.equal(call(buf[:need]), call(None)) and (buf[need:] == 99).all()
+
+
+def test_two_steps_at_once_on_two_streams():
+    """Calls on two streams share nothing: the same bits as one after the other."""
+    import torch
+    rng = np.random.default_rng(23)
+    I, J, T = 512, 256, 2000
+    b = mlp_buffers(rng, I, J, T, BF)
+    xs = [(dev(rng.standard_normal((T, J)), BF), dev(rng.standard_normal((T, J)), BF)) for _ in range(2)]
+    want = [mlp_step(b, X, dY, I, J, "gelu_tanh") for X, dY in xs]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [[], []]
+    for _ in range(3):
+        for k, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[k].append(mlp_step(b, *xs[k], I, J, "gelu_tanh"))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for g in got[k]:
+            assert all(torch.equal(g[n], want[k][n]) for n in ("H", "Y", "dWd", "dbd", "dZ", "dbu", "dWu", "dX", "kZ"))
+
+
+def test_infinities_and_nan_of_a_token_stay_with_it():
+    """Activations of infinite and NaN sums; other tokens keep their bits, in every kernel form that bf16 has."""
+    import torch
+    rng = np.random.default_rng(29)
+    for I, J, T, N, M in ((64, 4096, 4, 2, 4), (512, 264, 64, 2, 4), (64, 128, 1000, 2, 4), (1008, 136, 6200, 2, 4), (384, 200, 700, 4, 8)):
+        W, _ = masked_integers(rng, I, J, N, M)
+        v, idx = operand(np.abs(W), N, M, BF)
+        X = dev(few_ones(rng, T, J), BF)
+        for a, at_inf in (("relu", np.inf), ("gelu", np.inf), ("gelu_tanh", np.inf), ("silu", np.inf), ("none", np.inf)):
+            clean = bm.bimask_sparse_linear_fwd(X, v, idx, I, J, N, M, act=bm.ACTS[a])[0]
+            D = X.clone()
+            D[1], D[2] = 3e38, float("nan")                            # sums of like signs beyond bf16 and fp32: +inf
+            Y = bm.bimask_sparse_linear_fwd(D, v, idx, I, J, N, M, act=bm.ACTS[a])[0]
+            assert (Y[1] == at_inf).all() and torch.isnan(Y[2]).all(), (a, I)
+            keep = [t for t in range(T) if t not in (1, 2)]
+            assert torch.equal(Y[keep], clean[keep]), (a, I)
+
+
+def test_wrappers_refuse_what_does_not_fit():
+    """Types, sizes and layouts that the wrappers or the library refuse, and nothing is launched."""
+    import torch
+    rng = np.random.default_rng(31)
+    W, _ = masked_integers(rng, 64, 128, 2, 4)
+    v, idx = operand(W, 2, 4, BF)
+    X, R = dev(few_ones(rng, 6, 128), BF), dev(np.ones((6, 64)), BF)
+    f = lambda **k: bm.bimask_sparse_linear_fwd(**{**dict(X=X, Wf_values=v, Wf_index=idx, I=64, J=128, N=2, M=4), **k})  # noqa: E731
+    f()
+    for bad in (dict(J=64), dict(X=X.float()), dict(X=X.t()), dict(X=X.half()), dict(Wf_values=v[:-1]), dict(Wf_values=v.float()), dict(Wf_index=idx[:-1]), dict(bias=R[0].float()), dict(bias=R[0, :60]),
+                dict(residual=R.float()), dict(residual=R[:5]), dict(residual=R.t()), dict(Y=X), dict(ckpt=R), dict(ckpt=torch.zeros((6, 66, 2), dtype=torch.uint8, device="cuda")[:, :, 0])):
+        with pytest.raises((ValueError, TypeError)):
+            f(**bad)
+    for bad, status in ((dict(act=7), 5), (dict(ckpt=torch.zeros((65,), dtype=torch.uint8, device="cuda")), 6), (dict(I=62, Wf_values=v), 2), (dict(residual=R, Y=torch.as_strided(R, (6, 64), (64, 1), 0)[:6]), 0)):
+        if status == 0:
+            f(**bad)                                                   # the same memory under another name: in place
+            continue
+        with pytest.raises(bm.BimaskError) as e:
+            f(**bad)
+        assert e.value.status == status
+    ck = bm.bimask_checkpoint_store(X)
+    for call in (lambda: bm.bimask_checkpoint_store(X[0]), lambda: bm.bimask_checkpoint_store(X.half()), lambda: bm.bimask_checkpoint_load(ck.view(torch.int32), 6, 128), lambda: bm.bimask_checkpoint_load(ck, 6, 128, X=R),
+                 lambda: bm.bimask_act_bwd(R, ck, 1, dZ=X), lambda: bm.bimask_act_bwd(R, ck, 1, dbias=R[0]), lambda: bm.bimask_weight_grad(R, ck, 128, dW=R), lambda: bm.bimask_weight_grad(R, ck, 128, accumulate=True),
+                 lambda: bm.bimask_weight_grad(R.t(), ck, 128), lambda: bm.bimask_weight_grad(R, ck, 128, dw_dtype=torch.float16)):
+        with pytest.raises((ValueError, TypeError)):
+            call()
+    for call, status in ((lambda: bm.bimask_checkpoint_load(ck, 7, 128), 6), (lambda: bm.bimask_act_bwd(R, None, 2), 1), (lambda: bm.bimask_act_bwd(R, ck, 2, want_dZ=False, want_dbias=False), 1),
+                         (lambda: bm.bimask_weight_grad(R, ck, 129), 6), (lambda: bm.bimask_weight_grad(R.float(), ck, 128, dw_dtype=torch.bfloat16), 4), (lambda: bm.bimask_act_bwd(R[:1].expand(6, 64), ck, 0), 2)):
+        with pytest.raises(bm.BimaskError) as e:
+            call()
+        assert e.value.status == status

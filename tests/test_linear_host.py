@@ -140,3 +140,17 @@ def test_gpu_tests_reach_every_instance_of_the_kernels(rec):  # noqa: F811
     families = ("k_linear", "k_checkpoint", "k_act_bwd", "k_sum_strips", "k_sum_pieces", "k_weight_grad")
     missing = {k for k in rec.lib.stub_kernels().decode().splitlines() if k.startswith(families)} - names
     assert not missing, sorted(missing)
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    class Tensor:
+        is_cuda = True
+
+        def get_device(self):
+            return 1
+
+    monkeypatch.setattr(bm, "_device_index", lambda: 0)
+    with pytest.raises(ValueError, match="current device"):
+        bm._on_current_device(None, Tensor())
+    monkeypatch.setattr(bm, "_device_index", lambda: 1)
+    bm._on_current_device(Tensor(), None)
