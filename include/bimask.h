@@ -221,8 +221,11 @@ BIMASK_API int bimask_sparse_gemm_bwd(const void *dY, int64_t T, int64_t lddy, c
  * codes 0 and stands for 32 NaN.  The values are exact in both dtypes, and codes depend on the inputs alone.
  *
  * Errors of these calls are those of the others; in addition BIMASK_ERR_WORKSPACE for a checkpoint buffer smaller than
- * bimask_checkpoint_bytes says, BIMASK_ERR_UNSUPPORTED for an activation that does not exist and for outputs that overlap inputs
- * other than as stated.  T, C >= 1 (these matrices need not be multiples of M); pointers aligned to their elements unless stated;
+ * bimask_checkpoint_bytes says, BIMASK_ERR_UNSUPPORTED for an activation that does not exist and for outputs that overlap another
+ * argument other than as stated (Y may lie beside X or the residual in the rows of one buffer, dZ beside dY; any other output takes
+ * all that lies between its first and last element).  A workspace overlaps no other argument, which is not checked, and serves one
+ * call at a time: calls on two streams, or two captured graphs that may run together, need one each.  Nothing is kept in it.
+ * T, C >= 1 (these matrices need not be multiples of M); pointers aligned to their elements unless stated;
  * rows that start on 16 bytes take the fast path. */
 BIMASK_API size_t bimask_checkpoint_bytes(int64_t T, int64_t C);
 
@@ -234,6 +237,8 @@ BIMASK_API int bimask_checkpoint_load(const void *ckpt, size_t ckpt_bytes, int64
 
 /* Forward product with its epilogue:  Z = X (B .* W)^T + bias,  Y = act(Z) + residual.
  * Operands, layouts and alignments of bimask_sparse_gemm_fwd; sums, activation and residual in fp32, one rounding at the end.
+ * The activation is accurate to a few fp32 roundings; with bf16, BIMASK_ACT_GELU to 2^-12 of its tail min(Phi(z), 1 - Phi(z)) |z|.
+ * Activations of -infinity, where the formula is infinity * 0, are NaN or 0; a NaN stays a NaN.
  *   bias      in   I entries of dtype, 16-byte aligned, or NULL
  *   residual  in   T x I (ldr >= I; bf16: 4-byte aligned, even ldr) or NULL; may be Y itself (same pointer and leading dimension)
  *   ckpt      out  checkpoint of Z (T x I), from its fp32 values, or NULL                                                   */

@@ -318,10 +318,16 @@ int bimask_sparse_linear_fwd(const void* X, int64_t T, int64_t ldx, const void* 
         if (!(residual == Y && ldr == ldy) && !disjoint(residual, T, ldr, I, Y, ldy, I, esize(dtype))) return BIMASK_ERR_UNSUPPORTED;
     }
     if (!disjoint(X, T, ldx, J, Y, ldy, I, esize(dtype))) return BIMASK_ERR_UNSUPPORTED;
+    auto meets_operand = [&](const void* out, size_t bytes) {
+        return !apart(out, bytes, Wf_values, static_cast<size_t>(bimask_operand_elems(I, J, N, M)) * esize(dtype)) ||
+               (uses_sp24(N, M) && !apart(out, bytes, Wf_index, static_cast<size_t>(bimask_operand_index_words(I, J, N, M)) * 4)) ||
+               (bias && !apart(out, bytes, bias, static_cast<size_t>(I) * esize(dtype)));
+    };
+    if (meets_operand(Y, span(T, ldy, I, dtype))) return BIMASK_ERR_UNSUPPORTED;
     if (ckpt) {
         if (int rc = check_ckpt(ckpt, ckpt_bytes, T, I)) return rc;
         const size_t need = bimask_checkpoint_bytes(T, I);
-        if (!apart(ckpt, need, X, span(T, ldx, J, dtype)) || !apart(ckpt, need, Y, span(T, ldy, I, dtype)) ||
+        if (!apart(ckpt, need, X, span(T, ldx, J, dtype)) || !apart(ckpt, need, Y, span(T, ldy, I, dtype)) || meets_operand(ckpt, need) ||
             (residual && !apart(ckpt, need, residual, span(T, ldr, I, dtype)))) return BIMASK_ERR_UNSUPPORTED;
     }
     return launch_linear(Wf_values, Wf_index, I, J, uses_sp24(N, M), X, T, ldx, dtype, bias, act, residual, ldr, Y, ldy,
@@ -343,6 +349,9 @@ int bimask_act_bwd(const void* dY, int64_t T, int64_t lddy, const void* ckpt, si
     }
     if (dbias) {
         if (!aligned4(dbias)) return BIMASK_ERR_ALIGN;
+        const size_t out = static_cast<size_t>(I) * 4;
+        if (!apart(dbias, out, dY, span(T, lddy, I, dtype)) || (dZ && !apart(dbias, out, dZ, span(T, lddz, I, dtype))) ||
+            (ckpt && !apart(dbias, out, ckpt, need))) return BIMASK_ERR_UNSUPPORTED;
         const size_t ws = plan_act_bwd(T, I).ws_bytes;
         if (ws > 0 && (!workspace || workspace_bytes < ws)) return BIMASK_ERR_WORKSPACE;
         if (ws > 0 && !aligned16(workspace)) return BIMASK_ERR_ALIGN;

@@ -50,6 +50,12 @@ def test_linear_refusals(kw, want):
     assert lin(raw, **kw) == want
 
 
+@pytest.mark.parametrize("kw", [
+    dict(Y=B), dict(Y=B + 32 * 128 * 2 - 4), dict(Y=C + 4), dict(Y=C - 16 * 128), dict(bias=E, Y=E + 124), dict(bias=D + 32), dict(ck=B), dict(ck=C), dict(bias=E, ck=E - 32 * 66 + 16)])
+def test_linear_refuses_outputs_on_operands(kw):
+    assert lin(raw, **kw) == 5
+
+
 def test_linear_takes_what_it_documents(rec):  # noqa: F811
     for kw in (dict(), dict(bias=E), dict(R=E, ldr=64), dict(R=D, ldr=64), dict(R=E + 4, ldr=66), dict(ck=E, ckb=32 * 66), dict(R=D + 32 * 128, ldr=64), dict(idx=None, N=4, M=8),
                dict(Y=A + 2 * 128, ldx=192, ldy=192)):                             # (columns beside X in one buffer)
@@ -75,6 +81,11 @@ def act_bwd(f, dY=A, T=4000, lddy=64, ck=B, ckb=BIG, I=64, dtype=bm.BF16, act=2,
     (dict(wsb=16), 6), (dict(ws=E + 4), 7), (dict(db=D + 2), 7), (dict(ck=B + 4), 7), (dict(dZ=A + 2), 5), (dict(dZ=A, lddz=66), 5), (dict(dZ=B), 5), (dict(dY=A + 1), 7)])
 def test_act_bwd_refusals(kw, want):
     assert act_bwd(raw, **kw) == want
+
+
+@pytest.mark.parametrize("db", [A, A + 4000 * 128 - 4, B + 32, B + 4000 * 66 - 8, C + 256, C - 252])
+def test_act_bwd_refuses_a_bias_gradient_on_its_operands(db):
+    assert act_bwd(raw, db=db) == 5
 
 
 def test_act_bwd_launches(rec):  # noqa: F811
@@ -137,7 +148,7 @@ def test_gpu_tests_reach_every_instance_of_the_kernels(rec):  # noqa: F811
         assert st == 0
         reached.update(l)
     names = {f"{l.kernel}<{l.args}>" if l.args else l.kernel for l in reached}
-    families = ("k_linear", "k_checkpoint", "k_act_bwd", "k_sum_strips", "k_sum_pieces", "k_weight_grad")
+    families = ("k_linear", "k_checkpoint", "k_act_bwd", "k_sum_strips", "k_sum_pieces", "k_sum_few_pieces", "k_weight_grad")
     missing = {k for k in rec.lib.stub_kernels().decode().splitlines() if k.startswith(families)} - names
     assert not missing, sorted(missing)
 
