@@ -299,65 +299,84 @@ k_weight_grad(const uint16_t* __restrict__ dY, int64_t T, int64_t lddy, const ui
     }
 }
 
-// fp32: 64 x 64 tiles on four wavefronts, fp32 matrix instructions, whose operands are one element per lane: LDS rows as they lie.
-constexpr int kTileF32 = 64, kStageF32 = 32;
-__global__ void __launch_bounds__(256)
+// fp32: 64 x 64 tiles on 2 x 2 wavefronts, fp32 matrix instructions, whose operands are one element per lane: LDS rows as they lie.
+// A load of dY is one token's row for the whole wavefront, a buffer that ends with the row (or is empty beyond the last token); stages
+// are requested two ahead.  2048 x 2048 with 4096 tokens 322 us, 107 TFLOP/s (146 is what the matrix instructions reach without
+// anything beside them); 128 x 128 tiles, which read LDS half as often, 318, and 96 instead of 99 us at 1000 x 1000 with 4000: not
+// worth a second form.
+constexpr int kStageF32 = 32, kTileF32 = 64;
+__global__ void __launch_bounds__(256, 2)
 k_weight_grad_f32(const float* __restrict__ dY, int64_t T, int64_t lddy, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                   int64_t I, int64_t J, void* out, int64_t ldo, int mode, float* part, int tiles_j, int tiles, int64_t rows) {
-    __shared__ float sA[2][kStageF32][kTileF32 + 1], sB[2][kStageF32][kTileF32 + 1];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave & 1, wn = wave >> 1, l32 = lane & 31, h = lane >> 5;
-    const int n = blockIdx.x;
+    constexpr int B = kTileF32, PA = 8, PB = 2, WPR = B / 4;      // loads per thread and stage; words of codes per token
+    __shared__ f32x4 sA4[2][kStageF32 * B / 4], sB4[2][kStageF32 * B / 4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave & 1, wn = wave >> 1;
+    const int l32 = lane & 31, h = lane >> 5, n = blockIdx.x;
     if (n >= tiles) return;
-    const int64_t i0 = static_cast<int64_t>(n / tiles_j) * kTileF32, j0 = static_cast<int64_t>(n % tiles_j) * kTileF32;
+    const int64_t i0 = static_cast<int64_t>(n / tiles_j) * B, j0 = static_cast<int64_t>(n % tiles_j) * B;
     const int64_t t_begin = blockIdx.y * rows, t_end = t_begin + rows < T ? t_begin + rows : T;
     const int64_t pitch = ckpt_pitch(J), blocks = ckpt_blocks(J);
-    float ra[8];
-    uint32_t rb[2];
-    int rs[2];
-    auto load = [&](int64_t t0) {
+    const int row_bytes = static_cast<int>(I - i0 < B ? I - i0 : B) * 4;
+    const int64_t stages = t_begin < t_end ? ceil_div(t_end - t_begin, kStageF32) : 0;
+    float ra[2][PA];
+    uint32_t rb[2][PB];
+    int rs[2][PB];
+    auto load = [&](int set, int64_t st) {
+        const int64_t t0 = t_begin + st * kStageF32;
 #pragma unroll
-        for (int p = 0; p < 8; ++p) {                    // 4 token rows x 64 features at a time
-            const int64_t t = t0 + 4 * p + wave, i = i0 + lane;
-            ra[p] = t < t_end && i < I ? dY[t * lddy + i] : 0.f;
+        for (int p = 0; p < PA; ++p) {                   // wavefront w: rows w, w + 4, ...
+            const int64_t t = t0 + 4 * p + wave;
+            const auto A = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(dY + t * lddy + i0), 0, t < t_end ? row_bytes : 0, 0x00020000);
+            ra[set][p] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(A, 4 * lane, 0, 0));
         }
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {                    // 16 token rows x 64 codes at a time
-            const int64_t t = t0 + 16 * p + (tid >> 4), j = j0 + 4 * (tid & 15);
+        for (int p = 0; p < PB; ++p) {
+            const int q = tid + 256 * p, row = q / WPR;
+            const int64_t t = t0 + row, j = j0 + 4 * (q % WPR);
             const bool in = t < t_end && j < pitch;
-            rb[p] = in ? *reinterpret_cast<const uint32_t*>(codes + t * pitch + j) : 0u;
-            rs[p] = in ? scales[t * blocks + j / 32] : 0;
+            const uint32_t four = *reinterpret_cast<const uint32_t*>(codes + (in ? t * pitch + j : 0));
+            rs[set][p] = in ? scales[t * blocks + j / 32] : 0;
+            rb[set][p] = in ? four : 0u;
         }
     };
-    auto stage = [&](int s) {
+    auto stage = [&](int set, int buf) {
+        float* a = reinterpret_cast<float*>(sA4[buf]);
 #pragma unroll
-        for (int p = 0; p < 8; ++p) sA[s][4 * p + wave][lane] = ra[p];
+        for (int p = 0; p < PA; ++p) a[(4 * p + wave) * B + lane] = ra[set][p];
 #pragma unroll
-        for (int p = 0; p < 2; ++p)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sB[s][16 * p + (tid >> 4)][4 * (tid & 15) + e] = ckpt_value(rb[p], e, ckpt_scale(rs[p]));
+        for (int p = 0; p < PB; ++p) {
+            const float scale = ckpt_scale(rs[set][p]);
+            sB4[buf][tid + 256 * p] = (f32x4){ckpt_value(rb[set][p], 0, scale), ckpt_value(rb[set][p], 1, scale), ckpt_value(rb[set][p], 2, scale),
+                                              ckpt_value(rb[set][p], 3, scale)};
+        }
     };
     f32x16 acc;
 #pragma unroll
     for (int q = 0; q < 16; ++q) acc[q] = 0.f;
-    const int64_t stages = t_begin < t_end ? ceil_div(t_end - t_begin, kStageF32) : 0;
-    if (stages > 0) {
-        load(t_begin);
-        stage(0);
-    }
-    __syncthreads();
-    for (int64_t st = 0; st < stages; ++st) {
-        const int s = st & 1;
-        const bool more = st + 1 < stages;
-        if (more) load(t_begin + (st + 1) * kStageF32);
+    auto step = [&](auto set_c, int64_t st) {            // stage st lies in buffer `set`, stage st + 1 is on its way in the other set
+        constexpr int set = decltype(set_c)::value;
+        load(set, st + 2);
+        const float *a = reinterpret_cast<const float*>(sA4[set]) + 32 * wm + l32, *b = reinterpret_cast<const float*>(sB4[set]) + 32 * wn + l32;
 #pragma unroll
-        for (int k = 0; k < kStageF32; k += 2)
-            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(sA[s][k + h][32 * wm + l32], sB[s][k + h][32 * wn + l32], acc, 0, 0, 0);
-        if (more) stage(s ^ 1);
+        for (int k = 0; k < kStageF32; k += 2) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[(k + h) * B], b[(k + h) * B], acc, 0, 0, 0);
+        stage(set ^ 1, set ^ 1);
         __syncthreads();
+    };
+    if (stages > 0) {
+        load(0, 0);
+        load(1, 1);
+        stage(0, 0);
+        __syncthreads();
+#pragma unroll 1
+        for (int64_t st = 0; st < stages; st += 2) {     // (a stage beyond the last is one of zeros)
+            step(std::integral_constant<int, 0>{}, st);
+            step(std::integral_constant<int, 1>{}, st + 1);
+        }
     }
     const bool split = gridDim.y > 1;
     void* dst = split ? static_cast<void*>(part + static_cast<int64_t>(blockIdx.y) * I * J) : out;
-    const int64_t ld = split ? J : ldo, col = j0 + 32 * wn + l32;
+    const int64_t ld = split ? J : ldo;
+    const int64_t col = j0 + 32 * wn + l32;
     if (col < J)
 #pragma unroll
         for (int q = 0; q < 16; ++q) {
@@ -450,8 +469,11 @@ int run(const Operands& o, const WeightGradPlan& p) {
 // Tile and pieces.  A 256 x 256 tile moves half the LDS bytes of four 128 x 128 ones per product (2048 x 2048 with 4096 tokens 56 us
 // in 4 pieces of the 64 tiles, 61 with 256 tiles of 128 x 128; 1024 x 4096 with 8192 81 / 96), as long as tiles and pieces fill the 256
 // CUs once without much padding and a piece has the stages that pay for its sums (1024 x 1024 with 4096 34 / 30, 3000 x 1000 with 2000
-// 37 / 31).  Narrow matrices: tiles as narrow.  The others: two workgroups per CU are there at once, so at most 512, pieces of 16
-// stages or more, and none where the tiles alone fill half of the CUs (3000 x 1000 with 2000 tokens 31 us, in two pieces 35).
+// 37 / 31).  Narrow matrices: tiles as narrow.  The others: two workgroups per CU are there at once, so at most 512 pieces of tiles, and
+// none where the tiles alone fill half of the CUs (3000 x 1000 with 2000 tokens 31 us, in two pieces 35).  A piece's sums cost as much
+// as some stages, more of them the larger the matrix: at least 6 stages a piece with up to 16 tiles (200 x 200 with 3000 tokens 12.4 us,
+// with 16 stages 16.1), 16 with more (1000 x 1000 with 2000 24.3, with 8 stages 29).  fp32, whose stages take three times as long: pieces also up to
+// 256 tiles (1000 x 1000 with 4000 99 us, without 125), of 2 stages up to 64 tiles (100 x 100 with 1000 9.3, with 8 stages 14.7), then 8 (1024 x 512 with 200 11.8 / 15.3).
 WeightGradPlan plan_weight_grad(int64_t T, int64_t I, int64_t J, int dtype) {
     WeightGradPlan p;
     int64_t bm, bn, stage = kStageT, pieces;
@@ -473,7 +495,7 @@ WeightGradPlan plan_weight_grad(int64_t T, int64_t I, int64_t J, int dtype) {
     }
     const int64_t stages = ceil_div(T, stage), tiles = ceil_div(I, bm) * ceil_div(J, bn), large = ceil_div(I, 256) * ceil_div(J, 256);
     pieces = tiles >= 128 ? 1 : 512 / tiles;
-    int64_t least = p.tile == WeightGradPlan::k128x128 ? 16 : 8;
+    const int64_t least = dtype == BIMASK_F32 ? (tiles <= 64 ? 2 : 8) : tiles <= 16 ? 6 : 16;
     if (p.tile == WeightGradPlan::k128x128) {
         const int64_t n = large >= 256 ? 1 : 256 / large;
         const double filled = static_cast<double>(I) * static_cast<double>(J) / (static_cast<double>(large) * 65536) *
@@ -482,10 +504,11 @@ WeightGradPlan plan_weight_grad(int64_t T, int64_t I, int64_t J, int dtype) {
             p.tile = WeightGradPlan::k256x256;
             pieces = n;
         }
-    } else if (p.tile == WeightGradPlan::k64x64) {
-        pieces = tiles > 256 ? 1 : 512 / tiles;
+    } else if (dtype == BIMASK_F32 && tiles <= 256) {
+        pieces = 512 / tiles;
     }
-    const int64_t most = stages / least > 1 ? stages / least : 1;
+    int64_t most = stages / least;
+    if (most < 1 || (dtype == BIMASK_F32 && stages < 8)) most = 1;
     pieces = pieces < most ? pieces : most;
     p.rows = ceil_div(stages, pieces) * stage;
     p.pieces = ceil_div(T, p.rows);
