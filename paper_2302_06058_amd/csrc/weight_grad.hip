@@ -301,9 +301,8 @@ k_weight_grad(const uint16_t* __restrict__ dY, int64_t T, int64_t lddy, const ui
 
 // fp32: 64 x 64 tiles on 2 x 2 wavefronts, fp32 matrix instructions, whose operands are one element per lane: LDS rows as they lie.
 // A load of dY is one token's row for the whole wavefront, a buffer that ends with the row (or is empty beyond the last token); stages
-// are requested two ahead.  2048 x 2048 with 4096 tokens 322 us, 107 TFLOP/s (146 is what the matrix instructions reach without
-// anything beside them); 128 x 128 tiles, which read LDS half as often, 318, and 96 instead of 99 us at 1000 x 1000 with 4000: not
-// worth a second form.
+// are requested two ahead.  2048 x 2048 with 4096 tokens 322 us, 107 TFLOP/s; 1000 x 1000 with 4000 99 us (one stage ahead, elements
+// compared one by one: 409 and 121).  128 x 128 tiles, which read LDS half as often: 318 and 96, not worth a second form.
 constexpr int kStageF32 = 32, kTileF32 = 64;
 __global__ void __launch_bounds__(256, 2)
 k_weight_grad_f32(const float* __restrict__ dY, int64_t T, int64_t lddy, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
