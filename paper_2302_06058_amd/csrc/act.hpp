@@ -54,7 +54,7 @@ __device__ __forceinline__ void apply_act(float (&z)[n], int act) {
                 p = __builtin_fmaf(p, a, -1.14626077f);
                 p = __builtin_fmaf(p, a, -1.0003591f);
                 // (Q of an infinity is 0 and of a NaN NaN; the factor beside it is finite, so that an infinity stays one)
-                z[i] = __builtin_fmaf(-__builtin_fminf(a, 3.4e38f), __builtin_amdgcn_exp2f(p), __builtin_fmaxf(z[i], 0.f));
+                z[i] = __builtin_fmaf(-__builtin_elementwise_minimum(a, 3.4e38f), __builtin_amdgcn_exp2f(p), __builtin_elementwise_maximum(z[i], 0.f));
             } else {
                 z[i] *= phi_cdf(z[i], gauss(z[i]));
             }
@@ -108,9 +108,18 @@ __host__ __device__ inline int64_t ckpt_blocks(int64_t cols) { return ceil_div(c
 
 constexpr int64_t kMaxTokens = int64_t(1) << 38;         // rows of the matrices around the product: sizes in bytes stay in 64 bits
 constexpr int kCkptNaN = 255;
-// The scale byte e + 127 of a block whose largest magnitude has these bits (sign cleared; a NaN orders above infinity).  127.5 is
-// 1.9921875 * 2^6, mantissa bits 0x7F0000: from there on the next power.  -126 <= e <= 121 keeps 2^e, 2^-e and 127 * 2^e normal.
-__device__ __forceinline__ int ckpt_scale_byte(uint32_t most) {
+// The largest magnitude of n values; a NaN stays one (an instruction takes two values, their signs off on the way).
+template <int n>
+__device__ __forceinline__ float ckpt_most(const float (&v)[n]) {
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < n; ++i) most = __builtin_elementwise_maximum(most, __builtin_fabsf(v[i]));
+    return most;
+}
+// The scale byte e + 127 of a block with this largest magnitude.  127.5 is 1.9921875 * 2^6, mantissa bits 0x7F0000: from there on the
+// next power.  -126 <= e <= 121 keeps 2^e, 2^-e and 127 * 2^e normal.
+__device__ __forceinline__ int ckpt_scale_byte(float largest) {
+    const uint32_t most = __builtin_bit_cast(uint32_t, largest) & 0x7FFFFFFFu;
     const int x = static_cast<int>(most >> 23);
     if (x == 255) return kCkptNaN;
     const int b = x - 6 + ((most & 0x7FFFFFu) >= 0x7F0000u ? 1 : 0);
@@ -126,18 +135,18 @@ template <int n>
 __device__ __forceinline__ void ckpt_encode(const float (&v)[n], int byte, uint32_t (&out)[n / 4]) {
     const bool bad = byte == kCkptNaN;
     const float inv = ckpt_inverse(bad ? 127 : byte);
+    uint32_t q[n];
+#pragma unroll
+    for (int i = 0; i < n; ++i) q[i] = __builtin_bit_cast(uint32_t, __builtin_fmaf(v[i], inv, 12582912.f));
+    if (byte == 248)                                     // e is kept to 121: up to 128 steps
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const int k = static_cast<int>(q[i] - 0x4B400000u);
+            q[i] = k > 127 ? 127u : k < -127 ? static_cast<uint32_t>(-127) : q[i];
+        }
 #pragma unroll
     for (int w = 0; w < n / 4; ++w) {
-        uint32_t q[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = __builtin_bit_cast(uint32_t, __builtin_fmaf(v[4 * w + i], inv, 12582912.f));
-        if (byte == 248)                                 // e is kept to 121: up to 128 steps
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int k = static_cast<int>(q[i] - 0x4B400000u);
-                q[i] = k > 127 ? 127u : k < -127 ? static_cast<uint32_t>(-127) : q[i];
-            }
-        const uint32_t lo = __builtin_amdgcn_perm(q[1], q[0], 0x0C0C0400u), hi = __builtin_amdgcn_perm(q[3], q[2], 0x0C0C0400u);
+        const uint32_t lo = __builtin_amdgcn_perm(q[4 * w + 1], q[4 * w], 0x0C0C0400u), hi = __builtin_amdgcn_perm(q[4 * w + 3], q[4 * w + 2], 0x0C0C0400u);
         out[w] = bad ? 0u : lo | hi << 16;
     }
 }

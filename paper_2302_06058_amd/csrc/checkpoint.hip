@@ -114,15 +114,10 @@ k_checkpoint_store(const raw* __restrict__ X, int64_t T, int64_t J, int64_t ldx,
         Row16<raw> x;
         x.load(X + p.t * ldx, c, J);
         float f[kPiece];
-        uint32_t most = 0;
 #pragma unroll
-        for (int i = 0; i < kPiece; ++i) {
-            f[i] = x.get(i);
-            const uint32_t a = __builtin_bit_cast(uint32_t, f[i]) & 0x7FFFFFFFu;
-            most = a > most ? a : most;
-        }
-        const uint32_t other = __shfl_xor(most, 1);
-        const int byte = ckpt_scale_byte(other > most ? other : most);
+        for (int i = 0; i < kPiece; ++i) f[i] = x.get(i);
+        const float most = ckpt_most(f);
+        const int byte = ckpt_scale_byte(__builtin_elementwise_maximum(most, __shfl_xor(most, 1)));
         uint32_t four[4];
         ckpt_encode(f, byte, four);
         const u32x4 out = {four[0], four[1], four[2], four[3]};

@@ -106,19 +106,13 @@ struct LinearOut {                                       // bf16
                         z[4 * c + e] = x[e] + __builtin_bit_cast(float, e & 1 ? b[2 * c + (e >> 1)] & 0xFFFF0000u : b[2 * c + (e >> 1)] << 16);
                 }
                 if (codes) {
-                    uint32_t most = 0, d[2];
+                    uint32_t d[2];
                     if (!in1)                            // (nothing of theirs is stored)
 #pragma unroll
                         for (int e = 0; e < 8; ++e) z[e] = in0 && e < 4 ? z[e] : 0.f;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const uint32_t m = __builtin_bit_cast(uint32_t, z[e]) & 0x7FFFFFFFu;
-                        most = m > most ? m : most;
-                    }
-                    uint32_t o = __builtin_amdgcn_mov_dpp(most, 0xB1, 0xF, 0xF, true);       // the other lane of a pair, the other pair of four
-                    most = o > most ? o : most;
-                    o = __builtin_amdgcn_mov_dpp(most, 0x4E, 0xF, 0xF, true);
-                    most = o > most ? o : most;
+                    float most = ckpt_most(z);           // with the other lane of a pair, then the other pair of four
+                    most = __builtin_elementwise_maximum(most, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, most), 0xB1, 0xF, 0xF, true)));
+                    most = __builtin_elementwise_maximum(most, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, most), 0x4E, 0xF, 0xF, true)));
                     const int byte = ckpt_scale_byte(most);
                     ckpt_encode(z, byte, d);
                     if (a < pitch) {
@@ -163,13 +157,15 @@ struct LinearOut {                                       // bf16
     __device__ __forceinline__ void start(ACC& z, int lane, int a, int Adim) const {
         typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
         const int h = lane >> 5;
+        ACC v;                                           // (a new value: elements put into the old one would keep it alive until here)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             u32x2 b = {0u, 0u};
             if (bias && a + 8 * q + 4 * h < Adim) b = *reinterpret_cast<const u32x2*>(bias + a + 8 * q + 4 * h);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) z[4 * q + e] = __builtin_bit_cast(float, e & 1 ? b[e >> 1] & 0xFFFF0000u : b[e >> 1] << 16);
+            for (int e = 0; e < 4; ++e) v[4 * q + e] = __builtin_bit_cast(float, e & 1 ? b[e >> 1] & 0xFFFF0000u : b[e >> 1] << 16);
         }
+        z = v;
     }
     template <bool AHEAD, class ACC>
     __device__ __forceinline__ void before_rounding(ACC& z0, ACC& z1, Piece (&ahead)[4], bool more, uint8_t* strip, int lane, int a0, int64_t t0, int rows,
@@ -196,17 +192,13 @@ struct LinearOut {                                       // bf16
 #pragma unroll
             for (int q = 0; q < 16; ++q) y[q] = z[q];
             if (codes && a0 + 32 * i < Adim) {
-                uint32_t most = 0, d[4];
+                uint32_t d[4];
                 if (a0 + 32 * i + 32 > Adim)             // uniform, the last tile: features that do not exist count as 0
 #pragma unroll
                     for (int q = 0; q < 16; ++q) y[q] = a0 + 32 * i + 8 * (q >> 2) + 4 * h < Adim ? y[q] : 0.f;
-#pragma unroll
-                for (int q = 0; q < 16; ++q) {
-                    const uint32_t m = __builtin_bit_cast(uint32_t, y[q]) & 0x7FFFFFFFu;
-                    most = m > most ? m : most;
-                }
+                const uint32_t most = __builtin_bit_cast(uint32_t, ckpt_most(y));
                 const auto both = __builtin_amdgcn_permlane32_swap(most, most, false, false);
-                byte[i] = ckpt_scale_byte(both[0] > both[1] ? both[0] : both[1]);
+                byte[i] = ckpt_scale_byte(__builtin_elementwise_maximum(__builtin_bit_cast(float, static_cast<uint32_t>(both[0])), __builtin_bit_cast(float, static_cast<uint32_t>(both[1]))));
                 ckpt_encode(y, byte[i], d);
                 const auto lo = __builtin_amdgcn_permlane32_swap(d[0], d[2], false, false);
                 const auto hi = __builtin_amdgcn_permlane32_swap(d[1], d[3], false, false);
@@ -230,8 +222,10 @@ struct LinearOut {                                       // bf16
                     }
                 }
             }
+            ACC v;
 #pragma unroll
-            for (int q = 0; q < 16; ++q) z[q] = y[q];
+            for (int q = 0; q < 16; ++q) v[q] = y[q];
+            z = v;
             __builtin_amdgcn_sched_barrier(0);
         };
         half(z0, 0);
@@ -261,12 +255,9 @@ struct LinearOutF32 {
         float z[1] = {in && bias ? s + bias[a] : s};
         if (codes) {
             const float v = a < Adim ? z[0] : 0.f;
-            uint32_t most = __builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu;
+            float most = __builtin_fabsf(v);
 #pragma unroll
-            for (int x = 16; x > 0; x >>= 1) {
-                const uint32_t o = __shfl_xor(most, x);
-                most = o > most ? o : most;
-            }
+            for (int x = 16; x > 0; x >>= 1) most = __builtin_elementwise_maximum(most, __shfl_xor(most, x));
             const int byte = ckpt_scale_byte(most);
             float v4[4] = {v, 0.f, 0.f, 0.f};
             uint32_t code[1];
