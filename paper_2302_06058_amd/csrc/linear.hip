@@ -1,6 +1,12 @@
 // The linear layer's product with its epilogue:  Z = X (B .* W)^T + bias,  Y = act(Z) + residual  (operand of Eq. (3),
 // arXiv 2302.06058), on request with Z's 8-bit checkpoint.  linear_epilogue.hpp holds the epilogue; the main loops are those of
 // the plain products (gemm_sp24_body.hpp, gemm_sp24_big_body.hpp, gemm_sp24_wide_body.hpp, gemm_f32_body.hpp).
+//
+// What bounds it: a few tokens, the weights' bytes (11008 x 4096 at one token 10.5 us for 50.7 MB, 4.8 TB/s; 4096 x 11008 at 13 tokens 12.5);
+// the largest products, the plain product's own bound (11008 x 4096 at 8192 tokens with silu and checkpoint 470-550 us by the card's clock,
+// the plain product 390-460 beside it); short contractions, the instructions of the epilogue beside the matrix instructions (1536 x 384 at
+// 25216 tokens, 4:8 with gelu and checkpoint 60-66 us: the vector units issue 60 % of the time and the matrix pipe is busy 33 %, and two
+// wavefronts per SIMD overlap little of the two; other wavefront priorities change nothing).
 #include "gemm_sp24_body.hpp"
 #include "gemm_sp24_big_body.hpp"
 #include "gemm_sp24_wide_body.hpp"
@@ -88,10 +94,13 @@ int run_wide(const Problem& p, const LinearOut& out, const WidePlan& w) {
     return check_launch();
 }
 
-// Short contractions and wide outputs: the epilogue is most of the work there, and in this kernel it is each wavefront's own.
+// Short contractions and wide outputs: the epilogue is most of the work there, and in this kernel it is each wavefront's own.  Against the
+// forms below, us: 1536 x 384 at 25216 tokens with gelu and checkpoint 60.0 / 72.4, with residual 45.5 / 53.6, 4:8 with silu 46.9 / 63.7;
+// 384 x 384 19.8 / 22.4; 2048 x 512 at 2048 10.2 / 11.1.  Below 2^22 outputs its first rows arrive too late (512 x 512 at 2048 9.1 / 6.2,
+// 2048 x 512 at 1024 9.6 / 8.6), up to 256 features most of its wavefronts have nothing to do (128 x 512 at 25216 17.0 / 10.8).
 template <bool DENSE>
 int run_short(const Problem& p, const LinearOut& out) {
-    if (p.K > 512 || p.K % 8 || p.Adim % 8 || p.Adim <= 256 || p.T < 2048 || p.T > 0x7FFFFFFF || p.ldc >= (1 << 28)) return BIMASK_ERR_UNSUPPORTED;
+    if (p.K > 512 || p.K % 8 || p.Adim % 8 || p.Adim <= 256 || p.T < 2048 || p.Adim < ((1 << 22) + p.T - 1) / p.T || p.T > 0x7FFFFFFF || p.ldc >= (1 << 28)) return BIMASK_ERR_UNSUPPORTED;
     if (!aligned16(p.Bm) || !aligned16(p.C) || p.ldb % 8 || p.ldc % 8 || (out.R && !out.vecR)) return BIMASK_ERR_UNSUPPORTED;
     WidePlan p2, p4;
     const double us2 = wide_plan(2, p.Adim, p.K, p.T, false, DENSE, p2), us4 = wide_plan(4, p.Adim, p.K, p.T, false, DENSE, p4);
