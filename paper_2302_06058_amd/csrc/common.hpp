@@ -272,6 +272,7 @@ struct WeightGradPlan {
     enum Tile { k128x128, k256x256, k64x192, k64x256, k256x64, k64x64 } tile;      // output tile (the last: fp32)
     int64_t rows;        // tokens of a piece
     int64_t pieces;
+    int64_t first;       // 0, or: this plan is for so many rows of dW, the others take a plan of their own in a second launch
     size_t ws_bytes;     // sums of the pieces
 };
 WeightGradPlan plan_weight_grad(int64_t T, int64_t I, int64_t J, int dtype);

@@ -478,8 +478,12 @@ int run(const Operands& o, const WeightGradPlan& p) {
 // as some stages, more of them the larger the matrix: at least 6 stages a piece with up to 16 tiles (200 x 200 with 3000 tokens 12.4 us,
 // with 16 stages 16.1), 16 with more (1000 x 1000 with 2000 24.3, with 8 stages 29).  fp32, whose stages take three times as long: pieces also up to
 // 256 tiles (1000 x 1000 with 4000 99 us, without 125), of 2 stages up to 64 tiles (100 x 100 with 1000 9.3, with 8 stages 14.7), then 8 (1024 x 512 with 200 11.8 / 15.3).
+// More large tiles than CUs: where the last round over the chip would be at most half full, large tiles take the whole rounds and the rows
+// behind them a plan of their own, smaller tiles or pieces (4352 x 4096 with 4096 tokens, 272 tiles, 216 us in 128 x 128 tiles, 157 so;
+// 4864 x 4096 with 8192, 304, 421 / 308; 6144 x 4096 with 4096, 384, 219 / 211; but 5120 x 5120, 400, 222 / 247).
 WeightGradPlan plan_weight_grad(int64_t T, int64_t I, int64_t J, int dtype) {
     WeightGradPlan p;
+    p.first = 0;
     int64_t bm, bn, stage = kStageT, pieces;
     if (dtype == BIMASK_F32) {
         p.tile = WeightGradPlan::k64x64;
@@ -508,6 +512,16 @@ WeightGradPlan plan_weight_grad(int64_t T, int64_t I, int64_t J, int dtype) {
             p.tile = WeightGradPlan::k256x256;
             pieces = n;
         }
+        const int64_t across = ceil_div(J, 256), whole = large / 256 * 256, bands = whole / across, rest = large - bands * across;
+        if (whole > 0 && rest > 0 && rest <= 128 && stages >= 24 && bands * across * 10 >= whole * 9 && J * 8 >= across * 256 * 7) {
+            p.first = bands * 256;
+            if (I - p.first < 8) p.first -= 256;         // (fewer than 8 rows have no fast form)
+            p.tile = WeightGradPlan::k256x256;
+            p.pieces = 1;
+            p.rows = stages * stage;
+            p.ws_bytes = plan_weight_grad(T, I - p.first, J, dtype).ws_bytes;
+            return p;
+        }
     } else if (dtype == BIMASK_F32 && tiles <= 256) {
         pieces = 512 / tiles;
     }
@@ -535,6 +549,13 @@ int launch_weight_grad(const void* dY, int64_t T, int64_t lddy, const uint8_t* c
         rc = check_launch();
     } else {
         if (I < 8 || lddy >= (1 << 24) || J >= (1 << 25) || T >= (1ll << 31)) rc = run<128, 128, 2, 2, 2, false>(o, p);
+        else if (p.first > 0) {
+            Operands f = o;
+            f.I = p.first;
+            if (int rc1 = run<256, 256, 2, 4, 2, true>(f, p)) return rc1;
+            return launch_weight_grad(static_cast<const uint16_t*>(dY) + p.first, T, lddy, ckpt, I - p.first, J, dtype,
+                                      static_cast<uint8_t*>(dW) + p.first * lddw * (dw_dtype == BIMASK_BF16 ? 2 : 4), lddw, dw_dtype, accumulate, ws, s);
+        }
         else if (p.tile == WeightGradPlan::k256x256) rc = run<256, 256, 2, 4, 2, true>(o, p);
         else if (p.tile == WeightGradPlan::k64x192) rc = run<64, 192, 2, 2, 4, true>(o, p);
         else if (p.tile == WeightGradPlan::k64x256) rc = run<64, 256, 1, 4, 4, true>(o, p);

@@ -303,7 +303,8 @@ def test_not_a_number_in_a_checkpoint_reaches_the_gradient():
 # ---- weight gradient ------------------------------------------------------------------------------------------------------------------
 # (I, J, T, type of dY, type of dW, extra columns): every form of every kernel
 GRADS = [(1, 1, 1, BF, BF, 0), (8, 16, 3, BF, F32, 0), (33, 147, 65, BF, BF, 0), (64, 576, 5000, BF, F32, 0), (128, 128, 64, BF, BF, 8), (130, 1000, 257, BF, F32, 3), (1000, 72, 700, BF, BF, 0),
-         (4096, 3336, 96, BF, BF, 0), (4097, 3300, 130, BF, F32, 1), (64, 148, 20011, BF, BF, 0), (1000, 40, 700, BF, BF, 0), (301, 64, 9000, BF, F32, 1), (5, 300, 9000, BF, F32, 0), (15, 65, 33, BF, BF, 0), (40, 500, 300, BF, BF, 0), (505, 512, 49999, BF, F32, 0), (1031, 131, 5000, BF, BF, 0), (1, 3, 9000, BF, F32, 0), (3, 1, 20000, F32, F32, 0), (8, 300, 31, BF, BF, 1), (1, 1, 1, F32, F32, 0), (65, 130, 40, F32, F32, 0), (64, 128, 32, F32, F32, 4), (200, 96, 3000, F32, F32, 1)]
+         (4096, 3336, 96, BF, BF, 0), (4097, 3300, 130, BF, F32, 1), (64, 148, 20011, BF, BF, 0), (1000, 40, 700, BF, BF, 0), (301, 64, 9000, BF, F32, 1), (5, 300, 9000, BF, F32, 0), (15, 65, 33, BF, BF, 0), (40, 500, 300, BF, BF, 0), (505, 512, 49999, BF, F32, 0), (1031, 131, 5000, BF, BF, 0), (1, 3, 9000, BF, F32, 0), (3, 1, 20000, F32, F32, 0), (8, 300, 31, BF, BF, 1), (1, 1, 1, F32, F32, 0), (65, 130, 40, F32, F32, 0), (64, 128, 32, F32, F32, 4), (200, 96, 3000, F32, F32, 1),
+         (4360, 4090, 770, BF, F32, 1), (4100, 4096, 770, BF, BF, 0), (2060, 8200, 800, BF, BF, 0)]      # whole rounds of large tiles, the rows behind them in a second launch
 
 
 @pytest.mark.parametrize("I,J,T,dtype,dw,pad", GRADS)

@@ -108,6 +108,21 @@ def test_weight_grad_refusals(kw, want):
     assert grad(raw, **kw) == want
 
 
+@pytest.mark.parametrize("I,J,first", [(4360, 4090, 4096), (4100, 4096, 3840), (5120, 5120, 0), (4096, 4096, 0), (11008, 4096, 0), (4352, 4096, 4096)])
+def test_rows_behind_the_whole_rounds_of_a_weight_gradient(rec, I, J, first):  # noqa: F811
+    """Two launches that cover dW once, and the second's sums where it splits the tokens; its workspace is what the call asks for."""
+    need = bm.workspace_bytes(bm.WS_WEIGHT_GRAD, I, J, 770, 0, bm.BF16, 0, 0)
+    assert need == (bm.workspace_bytes(bm.WS_WEIGHT_GRAD, I - first, J, 770, 0, bm.BF16, 0, 0) if first else need)
+    st, l = grad(rec, T=770, I=I, J=J, lddy=I, lddw=J, wsb=need)
+    assert st == 0
+    if first:
+        assert len(l) == (3 if need else 2) and l[0].kernel == "k_weight_grad" and l[1].kernel == "k_weight_grad"
+    else:
+        assert len([x for x in l if x.kernel == "k_weight_grad"]) == 1
+    if need:
+        assert grad(rec, T=770, I=I, J=J, lddy=I, lddw=J, wsb=need - 1)[0] == 6
+
+
 def test_wrappers_refuse_tensors_that_are_not_on_the_gpu():
     import torch
     x, b = torch.zeros((4, 64), dtype=torch.bfloat16), torch.zeros((4 * 66,), dtype=torch.uint8)
