@@ -5,8 +5,8 @@
 //   act_bwd   dZ = dY * act'(Z~),  dbias = sum over the tokens of dZ (fp32)
 //
 // All three are bound by memory: one pass, 16 features (half a block) per thread and step, 16-byte accesses.  8192 x 11008 bf16: store 51 us
-// and load 42 (273 MB each: 5.4 and 6.4 TB/s; the codes just written are partly still in the last-level cache), act_bwd with silu 94
-// (454 MB, 4.8 TB/s; a plain copy reaches 5.15) and 5 for the strips' sums.  With few rows the activation's slope counts: 6347 x 1000
+// and load 42 (273 MB each: 5.4 and 6.4 TB/s; the codes just written are partly still in the last-level cache), act_bwd with silu 88
+// (454 MB, 5.1 TB/s; a plain copy reaches 5.15) and 4 for the strips' sums.  With few rows the activation's slope counts: 6347 x 1000
 // with gelu 14 us for 32 MB, about 35 instructions for each of 6.3 million values on 800 workgroups.
 #include "act.hpp"
 
@@ -267,14 +267,17 @@ int launch_checkpoint_load(const uint8_t* ckpt, int64_t T, int64_t J, int dtype,
 }
 
 // Feature tiles of up to 256 (16 threads side by side, a row segment of 512 bytes of bf16), and strips of tokens so that about
-// 2048 workgroups exist, none with fewer than 2 steps (one request of loads).
+// 4096 workgroups exist (8192 x 11008 with silu 91.7 us, with 2048 96.8), none with fewer than 4 steps of rows (two requests) where that
+// leaves 1024 workgroups (50000 x 400 34.7, with 2 steps 37.4), 2 where it leaves 512 (6347 x 1000 15.4, with 4 15.8), else 1 (512 x 1000
+// 6.5, with 2 7.5).
 ActBwdPlan plan_act_bwd(int64_t T, int64_t I) {
     ActBwdPlan p;
     const int64_t per_row = ckpt_pitch(I) / kPiece;
     p.log2c = per_row >= 16 ? 4 : ilog2(static_cast<int>(per_row));
     p.tiles = ceil_div(per_row, int64_t(1) << p.log2c);
-    const int64_t step = kThreads >> p.log2c, most = ceil_div(T, 2 * step);
-    int64_t strips = ceil_div(2048, p.tiles);
+    const int64_t step = kThreads >> p.log2c;
+    const int64_t least = ceil_div(T, 4 * step) * p.tiles >= 1024 ? 4 : ceil_div(T, 2 * step) * p.tiles >= 512 ? 2 : 1, most = ceil_div(T, least * step);
+    int64_t strips = ceil_div(4096, p.tiles);
     strips = strips < most ? strips : most;
     p.rows = round_up(ceil_div(T, strips), step);
     p.strips = ceil_div(T, p.rows);
