@@ -223,8 +223,13 @@ k_sum_strips(const float* __restrict__ part, int strips, int64_t ld, int64_t I, 
     const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
     const int64_t c = static_cast<int64_t>(blockIdx.x) * 16 + x;         // (strips are as wide as whole blocks: in bounds)
     float s = 0.f;
-#pragma unroll 4
-    for (int k = y; k < strips; k += 16) s += part[k * ld + c];
+    for (int k = y; k < strips; k += 16 * 8) {           // eight requests at once, those beyond the last strip of one that exists
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = part[(k + 16 * u < strips ? k + 16 * u : k) * ld + c];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += k + 16 * u < strips ? v[u] : 0.f;
+    }
     sums[y][x] = s;
     __syncthreads();
     if (y == 0 && c < I) {

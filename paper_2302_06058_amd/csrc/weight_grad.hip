@@ -428,10 +428,14 @@ k_sum_pieces(const float* __restrict__ part, int pieces, int64_t I, int64_t J, v
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * 64; first < total; first += static_cast<int64_t>(gridDim.x) * 64) {
         const int64_t e = first + x;
         float s = 0.f;
-        if (e < total) {
-#pragma unroll 8
-            for (int k = y; k < pieces; k += 4) s += part[k * total + e];
-        }
+        if (e < total)
+            for (int k = y; k < pieces; k += 4 * 12) {   // twelve requests at once, those beyond the last piece of one that exists
+                float v[12];
+#pragma unroll
+                for (int u = 0; u < 12; ++u) v[u] = part[(k + 4 * u < pieces ? k + 4 * u : k) * total + e];
+#pragma unroll
+                for (int u = 0; u < 12; ++u) s += k + 4 * u < pieces ? v[u] : 0.f;
+            }
         sums[y][x] = s;
         __syncthreads();
         if (y == 0 && e < total) {
