@@ -237,7 +237,7 @@ BIMASK_API int bimask_checkpoint_load(const void *ckpt, size_t ckpt_bytes, int64
 
 /* Forward product with its epilogue:  Z = X (B .* W)^T + bias,  Y = act(Z) + residual.
  * Operands, layouts and alignments of bimask_sparse_gemm_fwd; sums, activation and residual in fp32, one rounding at the end.
- * The activation is accurate to a few fp32 roundings; with bf16, BIMASK_ACT_GELU to 2^-12 of its tail min(Phi(z), 1 - Phi(z)) |z|.
+ * The activation is accurate to a few fp32 roundings.
  * Activations of -infinity, where the formula is infinity * 0, are NaN or 0; a NaN stays a NaN.
  *   bias      in   I entries of dtype, 16-byte aligned, or NULL
  *   residual  in   T x I (ldr >= I; bf16: 4-byte aligned, even ldr) or NULL; may be Y itself (same pointer and leading dimension)

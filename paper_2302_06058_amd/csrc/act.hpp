@@ -11,10 +11,7 @@ namespace bimask {
 // exactly 0 at both ends, where the other factors are finite.  gelu is z * Phi(z) with Phi's tail 0.5 erfc(|z| / sqrt 2) =
 // exp(-z^2 / 2) R(|z|); R (the Mills ratio over sqrt(2 pi)) as t * polynomial(t), t = 1 / (1 + 0.3 |z|): least squares on the
 // relative error, re-weighted to equal peaks, 1.5e-7 over 0 <= |z| <= 14.  The tail itself never comes from 1 - Phi.
-// COARSE, for results that are rounded to bf16 (2^-9): gelu as max(z, 0) - |z| Q(|z|), log2 Q a polynomial fitted over 0 .. 5.5 (Q off
-// by 2.5e-4 = 2^-12 of itself there; beyond, where Q < 2e-8, it keeps falling).  Slopes have no such form: the bias gradient that sums
-// them is fp32.
-// Cost of a value in issue slots (2^x and 1/x take four each): silu 11, gelu_tanh 13, gelu 24, coarse 12; slopes 12, 17, 25.
+// Cost of a value in issue slots (2^x and 1/x take four each): silu 11, gelu_tanh 13, gelu 24; slopes 12, 17, 25.
 constexpr float kLog2e = 1.44269504f, kTanhC1 = 1.5957691216f, kTanhC2 = 0.0713548163f;       // 2 sqrt(2/pi), times 0.044715
 
 __device__ __forceinline__ float sigma_of(float minus_u_log2e) {
@@ -37,7 +34,7 @@ __device__ __forceinline__ float phi_cdf(float z, float g) {
 }
 
 // z -> act(z), for n values; act is uniform
-template <bool COARSE, int n>
+template <int n>
 __device__ __forceinline__ void apply_act(float (&z)[n], int act) {
     if (act == BIMASK_ACT_NONE) return;
     if (act == BIMASK_ACT_RELU) {
@@ -45,20 +42,7 @@ __device__ __forceinline__ void apply_act(float (&z)[n], int act) {
         for (int i = 0; i < n; ++i) z[i] = z[i] <= 0.f ? 0.f : z[i];         // (NaN stays)
     } else if (act == BIMASK_ACT_GELU) {
 #pragma unroll
-        for (int i = 0; i < n; ++i) {
-            if constexpr (COARSE) {
-                const float a = __builtin_fabsf(z[i]);
-                float p = __builtin_fmaf(-2.33251254e-4f, a, 4.86977249e-3f);
-                p = __builtin_fmaf(p, a, -4.45990033e-2f);
-                p = __builtin_fmaf(p, a, -0.469681115f);
-                p = __builtin_fmaf(p, a, -1.14626077f);
-                p = __builtin_fmaf(p, a, -1.0003591f);
-                // (Q of an infinity is 0 and of a NaN NaN; the factor beside it is finite, so that an infinity stays one)
-                z[i] = __builtin_fmaf(-__builtin_elementwise_minimum(a, 3.4e38f), __builtin_amdgcn_exp2f(p), __builtin_elementwise_maximum(z[i], 0.f));
-            } else {
-                z[i] *= phi_cdf(z[i], gauss(z[i]));
-            }
-        }
+        for (int i = 0; i < n; ++i) z[i] *= phi_cdf(z[i], gauss(z[i]));
     } else if (act == BIMASK_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < n; ++i) z[i] *= sigma_of(-kLog2e * z[i]);

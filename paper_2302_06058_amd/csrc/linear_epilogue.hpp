@@ -122,7 +122,7 @@ struct LinearOut {                                       // bf16
                     dst_code += STEP * pitch;
                     dst_scale += STEP * (pitch / 32);
                 }
-                apply_act<true>(z, act);
+                apply_act(z, act);
                 u32x4 y;
 #pragma unroll
                 for (int d = 0; d < 4; ++d) {
@@ -205,7 +205,7 @@ struct LinearOut {                                       // bf16
                 if (l32 < rows)
                     *reinterpret_cast<u32x4*>(codes + t * ckpt_pitch(Adim) + a0 + 32 * i + 16 * h) = (u32x4){lo[0], lo[1], hi[0], hi[1]};
             }
-            apply_act<true>(y, act);
+            apply_act(y, act);
             if (R) {
 #pragma unroll
                 for (int p = 0; p < 2; ++p) {
@@ -269,7 +269,7 @@ struct LinearOutF32 {
             }
         }
         if (in) {
-            apply_act<false>(z, act);
+            apply_act(z, act);
             C[t * ldc + a] = R ? z[0] + R[t * ldr + a] : z[0];
         }
     }

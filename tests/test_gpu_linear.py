@@ -577,3 +577,36 @@ def test_wrappers_refuse_what_does_not_fit():
         with pytest.raises(bm.BimaskError) as e:
             call()
         assert e.value.status == status
+
+
+# ---- activations over their whole range ----------------------------------------------------------------------------------------------
+def range_of_z(dtype, n):
+    """n pre-activations that the type holds: every magnitude of bf16 from 2^-20 to 2^7, of fp32 as many, the largest ones and zeros."""
+    if dtype == BF:
+        z = (np.arange((127 - 20) << 7, (127 + 7) << 7, dtype=np.uint32) << 16).view(np.float32).astype(np.float64)
+    else:
+        rng = np.random.default_rng(37)
+        z = rounded(np.concatenate((np.exp2(rng.uniform(-20, 7, 6000)), rng.uniform(0, 15, 6000))), F32)
+    z = np.concatenate((z, -z, rounded([0.0, -0.0, 1e20, -1e20, 3e38, -3e38], dtype)))
+    return np.resize(z, n)
+
+
+def half_step(v, dtype):
+    """Half the distance of the type's values around v."""
+    bits = 7 if dtype == BF else 23
+    return 2.0 ** (np.floor(np.log2(np.maximum(np.abs(v), 2.0 ** -126))) - bits - 1)
+
+
+@pytest.mark.parametrize("a", ref.ACTS)
+@pytest.mark.parametrize("I,T,N,M,dtype", [(64, 120, 2, 4, BF), (512, 8200, 2, 4, BF), (512, 8200, 4, 8, BF), (64, 400, 2, 4, F32)])
+def test_activations_over_their_range(I, T, N, M, dtype, a):
+    """Weights that hand every feature through, nothing added: the activation alone, in the epilogues of the streaming, wide and fp32 kernels.
+    Relative error of function_error, and results below 2^-119 (where an exponential of fp32 ends) may be 0; then one rounding."""
+    v, idx = operand(np.eye(I), N, M, dtype)
+    z = range_of_z(dtype, T * I).reshape(T, I)
+    got = from_dev_f64(bm.bimask_sparse_linear_fwd(dev(z, dtype), v, idx, I, I, N, M, act=bm.ACTS[a])[0], dtype)
+    with np.errstate(over="ignore"):                                   # (1 + tanh(u)) / 2 = 1 / (1 + exp(-2u)), which loses no digits to 1 + tanh
+        want = z / (1.0 + np.exp(-np.sqrt(8.0 / np.pi) * (z + 0.044715 * z ** 3))) if a == "gelu_tanh" else ref.act(z, a)
+    off = 1.01 * ref.function_error(z, a) * np.abs(want) + (0.0 if a in ("none", "relu") else 2.0 ** -119)
+    bad = np.abs(got - want) > half_step(np.abs(want) + off, dtype) + off
+    assert not bad.any(), (bad.sum(), z[bad][:5], got[bad][:5], want[bad][:5])
