@@ -237,7 +237,8 @@ BIMASK_API int bimask_checkpoint_load(const void *ckpt, size_t ckpt_bytes, int64
 
 /* Forward product with its epilogue:  Z = X (B .* W)^T + bias,  Y = act(Z) + residual.
  * Operands, layouts and alignments of bimask_sparse_gemm_fwd; sums, activation and residual in fp32, one rounding at the end.
- * The activation is accurate to a few fp32 roundings.
+ * Before that rounding the activation is off by less than (32 + 3 u) 2^-24 of itself, u being the exponent it takes: z^2 / 2 for
+ * BIMASK_ACT_GELU, |z| for _SILU, 1.6 |z| + 0.072 |z|^3 for _GELU_TANH; below 2^-119 in magnitude it may be 0.
  * Activations of -infinity, where the formula is infinity * 0, are NaN or 0; a NaN stays a NaN.
  *   bias      in   I entries of dtype, 16-byte aligned, or NULL
  *   residual  in   T x I (ldr >= I; bf16: 4-byte aligned, even ldr) or NULL; may be Y itself (same pointer and leading dimension)
@@ -247,6 +248,7 @@ BIMASK_API int bimask_sparse_linear_fwd(const void *X, int64_t T, int64_t ldx, c
                              int64_t ldr, void *Y, int64_t ldy, void *ckpt, size_t ckpt_bytes, void *stream);
 
 /* Backward of the activation and the bias:  dZ = dY * act'(Z~),  dbias[i] = sum_t dZ[t][i], Z~ the values of Z's checkpoint.
+ * A slope is a sum of two terms, which may cancel; it is off like the activation above, by a share of the sum of their magnitudes.
  *   dY      in   T x I (lddy >= I), dtype
  *   ckpt    in   checkpoint of Z (T x I); may be NULL with BIMASK_ACT_NONE
  *   dZ      out  T x I (lddz >= I), dtype, or NULL; may be dY itself (same pointer and leading dimension)
