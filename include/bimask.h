@@ -226,7 +226,7 @@ BIMASK_API int bimask_sparse_gemm_bwd(const void *dY, int64_t T, int64_t lddy, c
  * all that lies between its first and last element).  A workspace overlaps no other argument, which is not checked, and serves one
  * call at a time: calls on two streams, or two captured graphs that may run together, need one each.  Nothing is kept in it.
  * T, C >= 1 (these matrices need not be multiples of M); pointers aligned to their elements unless stated;
- * rows that start on 16 bytes take the fast path. */
+ * rows that start on 16 bytes take the fast path.  bimask_checkpoint_bytes is 0 for sizes that the calls refuse (BIMASK_ERR_SHAPE). */
 BIMASK_API size_t bimask_checkpoint_bytes(int64_t T, int64_t C);
 
 /* X (T x C, ldx >= C, dtype) -> checkpoint, and back (X out: the values the checkpoint stands for). */

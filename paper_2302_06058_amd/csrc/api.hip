@@ -68,7 +68,9 @@ int check_rows(const void* p, int64_t T, int64_t C, int64_t ld, int dtype) {
 
 int check_ckpt(const void* ckpt, size_t bytes, int64_t T, int64_t C) {
     if (!ckpt) return BIMASK_ERR_NULL;
-    if (bytes < bimask_checkpoint_bytes(T, C)) return BIMASK_ERR_WORKSPACE;
+    const size_t need = bimask_checkpoint_bytes(T, C);
+    if (need == 0) return BIMASK_ERR_SHAPE;
+    if (bytes < need) return BIMASK_ERR_WORKSPACE;
     return aligned16(ckpt) ? BIMASK_OK : BIMASK_ERR_ALIGN;
 }
 
@@ -287,7 +289,7 @@ int bimask_sparse_gemm_bwd(const void* dY, int64_t T, int64_t lddy, const int32_
 }
 
 size_t bimask_checkpoint_bytes(int64_t T, int64_t C) {
-    if (T <= 0 || C <= 0 || T > kMaxTokens || C > 0x7FFFFFFFll) return 0;
+    if (T <= 0 || C <= 0 || T > kMaxTokens || C > 0x7FFFFFFFll || !sizes_fit(T, C)) return 0;
     return static_cast<size_t>(T) * static_cast<size_t>(ckpt_pitch(C) + ckpt_blocks(C));
 }
 

@@ -180,3 +180,10 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
         bm._on_current_device(None, Tensor())
     monkeypatch.setattr(bm, "_device_index", lambda: 1)
     bm._on_current_device(Tensor(), None)
+
+
+@pytest.mark.parametrize("T,J", [(1 << 38, 0x7FFFFFFF), (1 << 38, 1 << 30), (1 << 30, 1 << 28)])
+def test_checkpoints_too_large_to_count_are_refused(rec, T, J):  # noqa: F811
+    assert bm.checkpoint_bytes(T, J) == 0
+    assert grad(rec, T=T, I=4, J=J, lddy=4, lddw=J, ckb=16, wsb=1 << 62)[0] == 2
+    assert rec("bimask_checkpoint_load", B, 16, T, J, bm.F32, A, J, None)[0] == 2
