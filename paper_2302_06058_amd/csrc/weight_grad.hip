@@ -20,6 +20,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kStageT = 32;                              // tokens per stage
+constexpr int64_t kMaxStages = 1 << 30;                  // of a workgroup, counted (a few beyond the last too) in an int
 
 union Frag { bf16x8 v; u32x2 d[2]; };
 
@@ -542,6 +543,7 @@ int launch_weight_grad(const void* dY, int64_t T, int64_t lddy, const uint8_t* c
                        int dw_dtype, bool accumulate, float* ws, hipStream_t s) {
     const WeightGradPlan p = plan_weight_grad(T, I, J, dtype);
     const int mode = dw_dtype == BIMASK_BF16 ? (accumulate ? kAddBF16 : kOutBF16) : (accumulate ? kAddF32 : kOutF32);
+    if (p.rows > kMaxStages * kStageT) return BIMASK_ERR_SHAPE;
     const Operands o{dY, T, lddy, ckpt, ckpt + T * ckpt_pitch(J), I, J, dW, lddw, mode, ws, s};
     int rc;
     if (dtype == BIMASK_F32) {

@@ -187,3 +187,9 @@ def test_checkpoints_too_large_to_count_are_refused(rec, T, J):  # noqa: F811
     assert bm.checkpoint_bytes(T, J) == 0
     assert grad(rec, T=T, I=4, J=J, lddy=4, lddw=J, ckb=16, wsb=1 << 62)[0] == 2
     assert rec("bimask_checkpoint_load", B, 16, T, J, bm.F32, A, J, None)[0] == 2
+
+
+def test_weight_gradients_count_their_stages(rec):  # noqa: F811
+    """A workgroup counts its stages of 32 tokens in 31 bits: more than 2^30 of them are refused (no card holds such operands)."""
+    for T, want in ((1 << 35, 0), ((1 << 35) + 1, 2), (1 << 36, 2), (1 << 38, 2)):
+        assert grad(rec, dY=1 << 44, T=T, I=4, J=128 * 256, lddy=4, lddw=128 * 256, ck=1 << 54, ckb=1 << 62, dW=1 << 60, wsb=1 << 62)[0] == want
