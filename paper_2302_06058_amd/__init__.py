@@ -431,8 +431,10 @@ def _ckpt_buffer(ckpt, T: int, cols: int, like):
 
 
 def _workspace(workspace, need: int, like):
-    if workspace is None and need:
-        return _empty((need,), _torch.uint8, like)
+    if workspace is None:
+        return _empty((need,), _torch.uint8, like) if need else None
+    if not workspace.is_contiguous():
+        raise ValueError("a workspace is a contiguous tensor")
     return workspace
 
 
@@ -468,10 +470,11 @@ def bimask_sparse_linear_fwd(X, Wf_values, Wf_index, I: int, J: int, N: int, M: 
     ldx = _rows_of(X, "X", T, J, dtype)
     code = _dtype_code(X)
     slots = (I + 31) // 32 * ((J + 127) // 128) * 2048               # slot values of a 2-of-4 operand, a sixteenth as many index words
-    if Wf_values.dtype != dtype or Wf_values.numel() < (slots if N <= 2 else 2 * slots):
-        raise ValueError("Wf_values must hold the operand of an I x J matrix in the type of X")
-    if N <= 2 and Wf_index is not None and Wf_index.numel() * 16 < slots:
-        raise ValueError("Wf_index must hold the index words of an I x J matrix")
+    if Wf_values.dtype != dtype or Wf_values.numel() < (slots if N <= 2 else 2 * slots) or not Wf_values.is_contiguous():
+        raise ValueError("Wf_values must hold the operand of an I x J matrix, contiguous, in the type of X")
+    if N <= 2 and Wf_index is not None and (Wf_index.dtype not in (_torch.int32, _torch.uint32) or Wf_index.numel() * 16 < slots
+                                            or not Wf_index.is_contiguous()):
+        raise ValueError("Wf_index must hold the index words of an I x J matrix, contiguous, in 32 bits")
     ldr = 0
     if bias is not None:
         _vector(bias, "bias", I, dtype)

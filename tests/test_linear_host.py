@@ -193,3 +193,56 @@ def test_weight_gradients_count_their_stages(rec):  # noqa: F811
     """A workgroup counts its stages of 32 tokens in 31 bits: more than 2^30 of them are refused (no card holds such operands)."""
     for T, want in ((1 << 35, 0), ((1 << 35) + 1, 2), (1 << 36, 2), (1 << 38, 2)):
         assert grad(rec, dY=1 << 44, T=T, I=4, J=128 * 256, lddy=4, lddw=128 * 256, ck=1 << 54, ckb=1 << 62, dW=1 << 60, wsb=1 << 62)[0] == want
+
+
+@pytest.fixture
+def on_host(monkeypatch):
+    """Wrappers on host tensors, taken for those of the current device; every call of the library is recorded, none is made."""
+    import torch
+    calls = []
+
+    class Recorder:
+        def __getattr__(self, name):
+            if name.endswith("_bytes"):
+                return getattr(real, name)
+            return lambda *args: calls.append(name) or 0
+
+    real = bm.lib()
+    monkeypatch.setattr(bm, "_torch", torch)
+    monkeypatch.setattr(bm, "_device_index", lambda: -1)
+    monkeypatch.setattr(bm, "_raw_stream", lambda _: 0)
+    monkeypatch.setattr(bm, "lib", lambda: Recorder())
+    return calls
+
+
+def test_wrappers_refuse_operands_that_are_not_contiguous(on_host):
+    import torch
+    x = torch.zeros((6, 128), dtype=torch.bfloat16)
+    v, idx = torch.zeros((64 * 64,), dtype=torch.bfloat16), torch.zeros((64 * 4,), dtype=torch.int32)
+    bm.bimask_sparse_linear_fwd(x, v, idx, 64, 128, 2, 4)
+    bm.bimask_sparse_linear_fwd(x, v.view(32, -1), idx.view(torch.uint32).view(2, -1), 64, 128, 2, 4)
+    bm.bimask_sparse_linear_fwd(x, torch.zeros((64 * 128,), dtype=torch.bfloat16), None, 64, 128, 4, 8)
+    assert on_host == ["bimask_sparse_linear_fwd"] * 3
+    del on_host[:]
+    for values, index, N, M in ((v[:1].expand(64 * 64), idx, 2, 4), (torch.zeros((64 * 64, 2), dtype=torch.bfloat16)[:, 0], idx, 2, 4), (v, idx[:1].expand(64 * 4), 2, 4),
+                                (v, torch.zeros((64 * 4, 2), dtype=torch.int32)[:, 1], 2, 4), (v, idx.to(torch.int16), 2, 4), (v, idx.float(), 2, 4), (v, idx.to(torch.uint8), 2, 4), (v, idx.long(), 2, 4),
+                                (v[:1].expand(64 * 128), None, 4, 8)):
+        with pytest.raises(ValueError):
+            bm.bimask_sparse_linear_fwd(x, values, index, 64, 128, N, M)
+    assert not on_host
+
+
+def test_wrappers_refuse_workspaces_that_are_not_contiguous(on_host):
+    import torch
+    dY, ck = torch.zeros((4000, 64), dtype=torch.bfloat16), torch.zeros((4000 * 99,), dtype=torch.uint8)
+    for kind, call in ((bm.WS_ACT_BWD, lambda ws: bm.bimask_act_bwd(dY, None, bm.ACT_NONE, workspace=ws)), (bm.WS_WEIGHT_GRAD, lambda ws: bm.bimask_weight_grad(dY, ck, 96, workspace=ws))):
+        need = bm.workspace_bytes(kind, 64, 96, 4000, 0, bm.BF16, 0, 0)
+        assert need > 0
+        call(torch.zeros((need,), dtype=torch.uint8))
+        call(torch.zeros((need // 4,), dtype=torch.float32))
+        assert len(on_host) == 2
+        del on_host[:]
+        for ws in (torch.zeros((1,), dtype=torch.uint8).expand(need), torch.zeros((need, 2), dtype=torch.uint8)[:, 0], torch.zeros((2, need), dtype=torch.uint8)[:, ::2]):
+            with pytest.raises(ValueError):
+                call(ws)
+        assert not on_host
