@@ -613,3 +613,80 @@ def test_activations_over_their_range(I, T, N, M, dtype, a):
     off = 0.0 if a in ("none", "relu") else (32 + 3 * np.minimum(u, 120.0)) * 2.0 ** -24 * np.abs(want) + 2.0 ** -119
     bad = np.abs(got - want) > half_step(np.abs(want) + off, dtype) + off
     assert not bad.any(), (bad.sum(), z[bad][:5], got[bad][:5], want[bad][:5])
+
+
+# ---- ragged large products, blocks of zeros, infinities in checkpoints -----------------------------------------------------------------
+# (I, J, T, N, M, type): the streaming forms, split and not, both wide forms, the large form and fp32, the features no whole blocks of 32
+FORMS = [(100, 2184, 3, 2, 4, BF), (104, 648, 70, 4, 8, BF), (72, 128, 1000, 2, 4, BF), (520, 384, 8200, 2, 4, BF), (520, 384, 8200, 4, 8, BF), (1032, 1024, 21900, 2, 4, BF), (40, 64, 70, 2, 4, F32)]
+
+
+def exact_sums(X, W):
+    """X W^T of small integers: exact in fp32, whatever the order."""
+    return (X.astype(np.float32) @ W.astype(np.float32).T).astype(np.float64)
+
+
+def test_ragged_large_linear_is_exact():
+    """The large product with a last tile of 8 features and 12 tokens: every byte of output and checkpoint, a residual whose rows start on
+    4 bytes only, and in place."""
+    I, J, T, N, M, _ = FORMS[5]
+    rng = np.random.default_rng(41)
+    W, Wm = masked_integers(rng, I, J, N, M)
+    x, bias, res = few_ones(rng, T, J), rng.integers(-20, 21, I).astype(np.float64), rng.integers(-60, 61, (T, I)).astype(np.float64)
+    z = exact_sums(x, Wm) + bias
+    codes, scales = ref.store(z)
+    v, idx = operand(W, N, M, BF)
+    X, b = dev(x, BF), dev(bias[None], BF)[0]
+    for pad in (2, 8):                                                 # pitches of 4 and of 16 bytes
+        R, _ = strided(res, BF, pad)
+        Y, whole = strided(np.full((T, I), 99.0), BF, 8, 0, 99.0)
+        _, ck = bm.bimask_sparse_linear_fwd(X, v, idx, I, J, N, M, bias=b, residual=R, Y=Y, want_ckpt=True)
+        assert (from_dev_f64(Y, BF) == z + res).all()
+        gc, gs = ref.split(ck.cpu().numpy(), T, I)
+        assert (gc == codes).all() and (gs == scales).all()
+        Y.fill_(99.0)
+        assert (whole == 99.0).all(), "written beside or behind the rows"
+    bm.bimask_sparse_linear_fwd(X, v, idx, I, J, N, M, bias=b, act=bm.ACT_RELU, residual=R, Y=R)
+    assert (from_dev_f64(R, BF) == np.maximum(z, 0.0) + res).all()
+
+
+@pytest.mark.parametrize("I,J,T,N,M,dtype", FORMS)
+def test_blocks_of_zeros_have_the_smallest_scale(I, J, T, N, M, dtype):
+    rng = np.random.default_rng(43)
+    W, Wm = masked_integers(rng, I, J, N, M)
+    x = few_ones(rng, T, J)
+    x[1::3] = 0.0
+    v, idx = operand(W, N, M, dtype)
+    codes, scales = ref.store(exact_sums(x, Wm))
+    gc, gs = ref.split(bm.bimask_sparse_linear_fwd(dev(x, dtype), v, idx, I, J, N, M, want_ckpt=True)[1].cpu().numpy(), T, I)
+    assert (scales[1] == 1).all() and (gc == codes).all() and (gs == scales).all()
+    gc, gs = ref.split(bm.bimask_checkpoint_store(dev(x, dtype)).cpu().numpy(), T, J)
+    codes, scales = ref.store(x)
+    assert (gc == codes).all() and (gs == scales).all()
+
+
+@pytest.mark.parametrize("I,J,T,N,M,dtype", FORMS)
+def test_infinities_and_nan_reach_their_own_blocks_of_a_checkpoint(I, J, T, N, M, dtype):
+    """By token (its sums infinite or NaN) and by feature (an infinite bias): scale byte 255 and codes 0 there, no other byte changes."""
+    rng = np.random.default_rng(47)
+    W, _ = masked_integers(rng, I, J, N, M)
+    v, idx = operand(np.abs(W), N, M, dtype)
+    x, bias = few_ones(rng, T, J), np.ones(I)
+    call = lambda x, b: bm.bimask_sparse_linear_fwd(dev(x, dtype), v, idx, I, J, N, M, bias=dev(b[None], dtype)[0], act=bm.ACT_RELU, want_ckpt=True)  # noqa: E731
+    clean, k0 = call(x, bias)
+    c0, s0 = ref.split(k0.cpu().numpy(), T, I)
+    bad_x = x.copy()
+    bad_x[1], bad_x[T - 1] = 3e38, np.nan                              # sums of like signs beyond bf16 and fp32: +inf
+    keep = np.setdiff1d(np.arange(T), [1, T - 1])
+    Y, k = call(bad_x, bias)
+    c, s = ref.split(k.cpu().numpy(), T, I)
+    assert (s[[1, T - 1]] == 255).all() and (c[[1, T - 1]] == 0).all() and (c[keep] == c0[keep]).all() and (s[keep] == s0[keep]).all()
+    y, y0 = from_dev_f64(Y, dtype), from_dev_f64(clean, dtype)
+    assert np.isposinf(y[1]).all() and np.isnan(y[T - 1]).all() and (y[keep] == y0[keep]).all()
+    bias[I - 3] = -np.inf                                              # in the last block, which has features that do not exist
+    last = (I - 3) // 32
+    Y, k = call(x, bias)
+    c, s = ref.split(k.cpu().numpy(), T, I)
+    assert (s[:, last] == 255).all() and (c[:, 32 * last:32 * last + 32] == 0).all()
+    assert (s[:, :last] == s0[:, :last]).all() and (c[:, :32 * last] == c0[:, :32 * last]).all()
+    y = from_dev_f64(Y, dtype)
+    assert (y[:, I - 3] == 0).all() and (np.delete(y, I - 3, 1) == np.delete(y0, I - 3, 1)).all()
