@@ -26,7 +26,7 @@ __global__ void __launch_bounds__(64 * NW)
 k_gemm_f32(const float* __restrict__ A, const uint32_t* __restrict__ meta, int64_t Adim, int64_t K,
            const float* __restrict__ Bm, int64_t T, int64_t ldb, const int32_t* __restrict__ perm, float* __restrict__ C,
            int64_t ldc, uint32_t tiles_a, uint32_t tiles) {
-    gemm_f32_body<SPARSE, PERM, NW, R>(A, meta, Adim, K, Bm, T, ldb, perm, C, ldc, tiles_a, tiles, PlainOutF32{});
+    gemm_f32_body<SPARSE, PERM, NW, R>(A, meta, Adim, K, Bm, T, ldb, perm, C, ldc, tiles_a, tiles, PlainOut{});
 }
 
 template <bool SPARSE, bool PERM, int NW, int R>

@@ -1,19 +1,15 @@
 // Tile of the fp32 N:M GEMM for gfx950 (gemm_f32.hip states the design), shared by the plain product and the one with bias,
 // activation and residual.
 #pragma once
-#include "common.hpp"
+#include "mfma_types.hpp"
 
 namespace bimask {
 namespace {
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = 16;             // output tile: 16 weight rows x 16 tokens
 typedef f32x4 f32x4_row __attribute__((aligned(4)));      // 16 bytes of a token row: rows start on 4 bytes at least
 constexpr int64_t kManyTiles = 8192;  // 16 x 16 tiles from which a workgroup takes 64 weight rows (one step: 4 times as many)
 constexpr int64_t kTilesX = 1 << 20;  // tiles in the x dimension of a launch at most
-
-struct PlainOutF32 { static constexpr bool kFused = false; };
 
 // one 8-index piece of a weight row: SPARSE: decoded from 4 slot values and 16 index bits
 template <bool SPARSE>
@@ -51,7 +47,7 @@ __device__ __forceinline__ float weight_at(const WeightPiece<SPARSE>& w, int e) 
 // R: row tiles of a workgroup (16 R weight rows x 16 tokens); the token pieces are loaded once for all of them and the output
 // leaves in segments of 64 R bytes.  Token rows may start on any 4 bytes: the 16-byte loads need no more (256 x 256 at 50176
 // tokens, rows of 1028 bytes, 4:8: 254 us with 4-byte loads, 85).
-// OUT: what becomes of the sums (PlainOutF32: written).
+// OUT: what becomes of the sums (PlainOut: written).
 template <bool SPARSE, bool PERM, int NW, int R, class OUT>
 __device__ __forceinline__ void
 gemm_f32_body(const float* A, const uint32_t* meta, int64_t Adim, int64_t K, const float* Bm, int64_t T, int64_t ldb, const int32_t* perm,

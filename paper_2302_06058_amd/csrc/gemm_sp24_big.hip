@@ -31,8 +31,6 @@
 namespace bimask {
 namespace {
 
-struct PlainOut { static constexpr bool kFused = false; };
-
 __global__ void __launch_bounds__(kBigThreads)
 k_gemm_sp24_big(const uint16_t* __restrict__ A, const uint32_t* __restrict__ Ameta, int64_t Adim, int nk,
                 const uint16_t* __restrict__ Bm, int64_t T, int64_t ldb, uint16_t* __restrict__ C, int64_t ldc,

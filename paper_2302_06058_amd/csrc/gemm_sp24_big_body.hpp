@@ -1,16 +1,10 @@
 // Persistent large-problem loop of the 2:4 GEMM for gfx950 (gemm_sp24_big.hip states the design), shared by the plain product and the
 // one with bias, activation and residual.
 #pragma once
-#include "common.hpp"
+#include "mfma_types.hpp"
 
 namespace bimask {
 namespace {
-
-typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
-typedef __attribute__((__vector_size__(16 * sizeof(__bf16)))) __bf16 bf16x16;
-typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kBigThreads = 512;        // 8 wavefronts
 constexpr int kBigRows = 512;           // weight rows per workgroup tile
@@ -18,9 +12,6 @@ constexpr int kBigTokens = 128;         // tokens per full tile
 constexpr int kBigStage = kBigTokens * 256;          // LDS bytes of one token stage (128 k = 256 B per token)
 constexpr int kBigOut = kBigTokens * 512;            // LDS bytes of the output staging area (one pass of 256 weight rows)
 constexpr int kBigSmem = 2 * kBigStage + kBigOut;    // 128 KB: two token stages + output staging
-
-union BFragB { bf16x16 v; u32x4 q[2]; };
-union AFragB { bf16x8 v; u32x4 q; };
 
 // Work order.  One workgroup per CU, persistent: 256 workgroups, dealt round-robin to the 8 XCDs (each with its own
 // L2).  XCD x owns the contiguous run of `tpx` token tiles starting at x * tpx, against all weight tiles; the tiles
@@ -149,7 +140,7 @@ gemm_sp24_big_body(const uint16_t* A, const uint32_t* Ameta, int64_t Adim, int n
 #define BIMASK_BIG_MFMA(frag, s4v, j)                                                            \
     {                                                                                            \
         _Pragma("unroll") for (int i = 0; i < TM; ++i) {                                         \
-            AFragB af;                                                                           \
+            AFrag af;                                                                           \
             af.q = ra[i][s4v];                                                                   \
             const int idx = static_cast<int>((s4v) < 2 ? rmeta[i].x : rmeta[i].y);               \
             if ((s4v) & 1)                                                                       \
@@ -222,7 +213,7 @@ gemm_sp24_big_body(const uint16_t* A, const uint32_t* Ameta, int64_t Adim, int n
             wb[i] = weight_base(cw, i);
             rmeta_next[i] = *reinterpret_cast<const u32x2*>(index_base(cw, i) + l8);
         }
-        BFragB f[kDepth + 1];
+        BFrag f[kDepth + 1];
 #pragma unroll
         for (int d = 0; d < kDepth; ++d) BIMASK_BIG_FRAG(f[d], d / TN, d % TN)
 #pragma unroll

@@ -1,25 +1,13 @@
 // Main loop of the streaming N:M GEMM for gfx950 (gemm_sp24.hip states the design), shared by the plain product and the one
 // with bias, activation and residual.
 #pragma once
-#include "common.hpp"
+#include "mfma_types.hpp"
 
 namespace bimask {
 namespace {
 
-typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
-typedef __attribute__((__vector_size__(16 * sizeof(__bf16)))) __bf16 bf16x16;
-typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));   // native 16-byte register vector
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-
 constexpr int SK = 128;                 // dense k per stage
 constexpr int kRowBytes = SK * 2;       // LDS bytes per token row per stage (16 granules)
-
-union BFrag { bf16x16 v; u32x4 q[2]; };
-union AFrag { bf16x8 v; u32x4 q; };
-
-struct PlainOut { static constexpr bool kFused = false; };
 
 template <int BN, int KG>
 struct SpSmem {

@@ -16,8 +16,6 @@
 namespace bimask {
 namespace {
 
-struct PlainOut { static constexpr bool kFused = false; };
-
 template <int TN, bool DENSE>
 __global__ void __launch_bounds__(64 * kWideWaves, 2)
 k_gemm_sp24_wide(const uint16_t* __restrict__ A, const uint32_t* __restrict__ Ameta, int Adim, int K,

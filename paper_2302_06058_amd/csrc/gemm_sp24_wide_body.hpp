@@ -1,19 +1,10 @@
 // Main loop of the wide N:M GEMM for gfx950 (gemm_sp24_wide.hip states the design), shared by the plain product and the one with
 // bias, activation and residual.
 #pragma once
-#include "common.hpp"
+#include "mfma_types.hpp"
 
 namespace bimask {
 namespace {
-
-typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
-typedef __attribute__((__vector_size__(16 * sizeof(__bf16)))) __bf16 bf16x16;
-typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-
-union BFragV { bf16x16 v; bf16x8 half[2]; u32x4 q[2]; };
-union AFragV { bf16x8 v; u32x4 q; };
 
 constexpr int kWideLds = 160 * 1024;
 constexpr int kWideWaves = 8;
@@ -141,7 +132,7 @@ gemm_sp24_wide_body(const uint16_t* A, const uint32_t* Ameta, int Adim, int K, c
 #pragma unroll
         for (int x = 0; x < 2; ++x) fo[s4][x] = l32 * 256 + (((8 * x + 2 * s4 + h) ^ (l32 & 15)) << 4);
     constexpr int kDepth = 3, NQ = 4 * TN;                               // fragments read ahead; fragments of a stage
-    BFragV f[kDepth + 1];
+    BFrag f[kDepth + 1];
     auto read = [&](int stage, int q) {                                  // fragment q of a stage: sub-step q / TN, tokens 32 (q % TN) ..
         const uint8_t* p = smem + stage * (ROWS * 256) + (q % TN) * 8192;
         f[q % (kDepth + 1)].q[0] = *reinterpret_cast<const u32x4*>(p + fo[q / TN][0]);
@@ -175,8 +166,8 @@ gemm_sp24_wide_body(const uint16_t* A, const uint32_t* Ameta, int Adim, int K, c
                 read(q + kDepth < NQ ? st : st_next, (q + kDepth) % NQ);
 #pragma unroll
                 for (int i = 0; i < TM; ++i) {
-                    const BFragV& b = f[q % (kDepth + 1)];
-                    AFragV af;
+                    const BFrag& b = f[q % (kDepth + 1)];
+                    AFrag af;
                     if constexpr (DENSE) {
 #pragma unroll
                         for (int x = 0; x < 2; ++x) {

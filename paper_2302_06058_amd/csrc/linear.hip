@@ -16,12 +16,12 @@
 namespace bimask {
 namespace {
 
-template <int BM, int BN, int WAVES_M, int WAVES_N, int KG, int PF, bool BGUARD, bool BHALF, bool KTAIL, bool DENSE, int TR>
+template <int BM, int BN, int WAVES_M, int WAVES_N, int KG, int PF, bool BGUARD, bool KTAIL, bool DENSE, int TR>
 __global__ void __launch_bounds__(64 * WAVES_M * WAVES_N * KG)
 k_linear_sp24(const uint16_t* __restrict__ A, const uint32_t* __restrict__ Ameta, int64_t Adim, int64_t K,
               const uint16_t* __restrict__ Bm, int64_t T, int64_t ldb, uint16_t* C, int64_t ldc,
               int tiles_a, bool vecC, LinearOut out) {
-    gemm_sp24_body<BM, BN, WAVES_M, WAVES_N, KG, PF, BGUARD, BHALF, KTAIL, DENSE, TR>(A, Ameta, Adim, K, Bm, T, ldb, C, ldc, tiles_a, vecC, out);
+    gemm_sp24_body<BM, BN, WAVES_M, WAVES_N, KG, PF, BGUARD, false, KTAIL, DENSE, TR>(A, Ameta, Adim, K, Bm, T, ldb, C, ldc, tiles_a, vecC, out);
 }
 
 __global__ void __launch_bounds__(kBigThreads)
@@ -48,10 +48,10 @@ struct Problem {
     const void* A; const uint32_t* meta; int64_t Adim, K; const void* Bm; int64_t T, ldb; void* C; int64_t ldc; hipStream_t s;
 };
 
-template <int BM, int BN, int WAVES_M, int WAVES_N, int KG, int PF, bool BGUARD, bool BHALF, bool KTAIL, bool DENSE, int TR = BN>
+template <int BM, int BN, int WAVES_M, int WAVES_N, int KG, int PF, bool BGUARD, bool KTAIL, bool DENSE, int TR = BN>
 int run_t(const Problem& p, const LinearOut& out) {
     using S = SpSmem<BN, KG>;
-    auto kern = k_linear_sp24<BM, BN, WAVES_M, WAVES_N, KG, PF, BGUARD, BHALF, KTAIL, DENSE, TR>;
+    auto kern = k_linear_sp24<BM, BN, WAVES_M, WAVES_N, KG, PF, BGUARD, KTAIL, DENSE, TR>;
     if (S::kTotal > 48 * 1024) {
         static DeviceMemo attr_set;
         const int dev = DeviceMemo::device();
@@ -71,11 +71,11 @@ int run_t(const Problem& p, const LinearOut& out) {
 
 // (TR: token rows fetched, where the tile has more than there are)
 // rows: 0 whole stages of 16-byte token rows, 1 the last stage may end early (K a multiple of 8), 2 any rows (4-byte loads)
-template <int BM, int BN, int WAVES_M, int WAVES_N, int PF, bool BHALF, int KG, bool DENSE>
+template <int BM, int BN, int WAVES_M, int WAVES_N, int PF, int KG, bool DENSE>
 int run(const Problem& p, const LinearOut& out, int rows) {
-    if (rows == 0) return run_t<BM, BN, WAVES_M, WAVES_N, KG, PF, false, BHALF, false, DENSE>(p, out);
-    if (rows == 1) return run_t<BM, BN, WAVES_M, WAVES_N, KG, PF, false, BHALF, true, DENSE>(p, out);
-    return run_t<BM, BN, WAVES_M, WAVES_N, KG, 1, true, false, false, DENSE>(p, out);
+    if (rows == 0) return run_t<BM, BN, WAVES_M, WAVES_N, KG, PF, false, false, DENSE>(p, out);
+    if (rows == 1) return run_t<BM, BN, WAVES_M, WAVES_N, KG, PF, false, true, DENSE>(p, out);
+    return run_t<BM, BN, WAVES_M, WAVES_N, KG, 1, true, false, DENSE>(p, out);
 }
 
 template <int TN, bool DENSE>
@@ -169,23 +169,23 @@ int run_bf16(const Problem& p, const LinearOut& out) {
     const bool deep = p.K > (rows16 ? 256 : 384);
     if constexpr (!DENSE)
         if (p.K > 2048 && ceil_div(p.Adim, 32) * ceil_div(p.T, 32) <= 256) {
-            if (rows == 2) return run_t<32, 32, 1, 1, 8, 1, true, false, false, false>(p, out);
-            if (p.T <= 4) return run_t<32, 32, 1, 1, 8, 3, false, false, true, false, 4>(p, out);
-            if (p.T <= 16) return run_t<32, 32, 1, 1, 8, 2, false, false, true, false, 16>(p, out);
-            return run_t<32, 32, 1, 1, 8, 1, false, false, true, false>(p, out);
+            if (rows == 2) return run_t<32, 32, 1, 1, 8, 1, true, false, false>(p, out);
+            if (p.T <= 4) return run_t<32, 32, 1, 1, 8, 3, false, true, false, 4>(p, out);
+            if (p.T <= 16) return run_t<32, 32, 1, 1, 8, 2, false, true, false, 16>(p, out);
+            return run_t<32, 32, 1, 1, 8, 1, false, true, false>(p, out);
         }
     if (deep && gemm_few_tiles(p.Adim, p.T)) {
-        if constexpr (!DENSE) return run<64, 32, 2, 1, 1, false, 4, false>(p, out, rows);
+        if constexpr (!DENSE) return run<64, 32, 2, 1, 1, 4, false>(p, out, rows);
         // (the form for whole stages would not fit the registers)
-        else return rows == 2 ? run_t<64, 32, 2, 1, 4, 1, true, false, false, true>(p, out) : run_t<64, 32, 2, 1, 4, 1, false, false, true, true>(p, out);
+        else return rows == 2 ? run_t<64, 32, 2, 1, 4, 1, true, false, true>(p, out) : run_t<64, 32, 2, 1, 4, 1, false, true, true>(p, out);
     }
     if constexpr (!DENSE)
-        if (deep && p.Adim > 64 && ceil_div(p.Adim, 64) * ceil_div(p.T, 64) <= 256) return run<64, 64, 2, 2, 1, false, 2, false>(p, out, rows);
-    if (p.Adim <= 64) return run<64, 64, 2, 2, 2, false, 1, DENSE>(p, out, rows);
+        if (deep && p.Adim > 64 && ceil_div(p.Adim, 64) * ceil_div(p.T, 64) <= 256) return run<64, 64, 2, 2, 1, 2, false>(p, out, rows);
+    if (p.Adim <= 64) return run<64, 64, 2, 2, 2, 1, DENSE>(p, out, rows);
     const int64_t w256 = round_up(p.Adim, 256), w128 = round_up(p.Adim, 128);
     const bool narrow = (w256 - w128) * 5 >= w256, big = ceil_div(p.Adim, 256) * ceil_div(p.T, 128) >= 190;
-    if (!narrow && big) return run<256, 128, 8, 1, 1, false, 1, DENSE>(p, out, rows);
-    return run<128, 64, 4, 1, 2, false, 1, DENSE>(p, out, rows);
+    if (!narrow && big) return run<256, 128, 8, 1, 1, 1, DENSE>(p, out, rows);
+    return run<128, 64, 4, 1, 2, 1, DENSE>(p, out, rows);
 }
 
 }  // namespace
