@@ -3,10 +3,10 @@
 // the plain products (gemm_sp24_body.hpp, gemm_sp24_big_body.hpp, gemm_sp24_wide_body.hpp, gemm_f32_body.hpp).
 //
 // What bounds it: a few tokens, the weights' bytes (11008 x 4096 at one token 10.5 us for 50.7 MB, 4.8 TB/s; 4096 x 11008 at 13 tokens 12.5);
-// the largest products, the plain product's own bound (11008 x 4096 at 8192 tokens with silu and checkpoint 470-550 us by the card's clock,
+// the largest products, the plain product's own bound (11008 x 4096 at 8192 tokens with silu and checkpoint 460-530 us by the card's clock,
 // the plain product 390-460 beside it); short contractions, the instructions of the epilogue beside the matrix instructions (1536 x 384 at
-// 25216 tokens, 4:8 with gelu and checkpoint 60-66 us: the vector units issue 60 % of the time and the matrix pipe is busy 33 %, and two
-// wavefronts per SIMD overlap little of the two; other wavefront priorities change nothing).
+// 25216 tokens, 4:8 with gelu and checkpoint 74-78 us, with silu 55: the vector units issue 71 % of the time with gelu and the matrix pipe is
+// busy 27 %, and two wavefronts per SIMD overlap little of the two; other wavefront priorities change nothing).
 #include "gemm_sp24_body.hpp"
 #include "gemm_sp24_big_body.hpp"
 #include "gemm_sp24_wide_body.hpp"
@@ -95,9 +95,9 @@ int run_wide(const Problem& p, const LinearOut& out, const WidePlan& w) {
 }
 
 // Short contractions and wide outputs: the epilogue is most of the work there, and in this kernel it is each wavefront's own.  Against the
-// forms below, us: 1536 x 384 at 25216 tokens with gelu and checkpoint 60.0 / 72.4, with residual 45.5 / 53.6, 4:8 with silu 46.9 / 63.7;
-// 384 x 384 19.8 / 22.4; 2048 x 512 at 2048 10.2 / 11.1.  Below 2^22 outputs its first rows arrive too late (512 x 512 at 2048 9.1 / 6.2,
-// 2048 x 512 at 1024 9.6 / 8.6), up to 256 features most of its wavefronts have nothing to do (128 x 512 at 25216 17.0 / 10.8).
+// forms below, us: 1536 x 384 at 25216 tokens, 4:8 with gelu and checkpoint 75 / 92, 2:4 66 / 81, with residual 44 / 54, 4:8 with silu 47 / 68;
+// 384 x 384 with gelu and checkpoint 23.0 / 24.2, as 2048 x 512 at 2048 11.2 / 11.6.  Below 2^22 outputs its first rows arrive too late (512 x 512
+// at 2048 9.8 / 7.6, 2048 x 512 at 1024 10.5 / 9.0), up to 256 features most of its wavefronts have nothing to do (128 x 512 at 25216 19.0 / 11.3).
 template <bool DENSE>
 int run_short(const Problem& p, const LinearOut& out) {
     if (p.K > 512 || p.K % 8 || p.Adim % 8 || p.Adim <= 256 || p.T < 2048 || p.Adim < ((1 << 22) + p.T - 1) / p.T || p.T > 0x7FFFFFFF || p.ldc >= (1 << 28)) return BIMASK_ERR_UNSUPPORTED;

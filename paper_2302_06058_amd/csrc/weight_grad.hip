@@ -67,9 +67,9 @@ constexpr int kGradLds = 3 * kStageT * (BM + BN) * 2 > WM * WN * 32 * (BN / WN +
 // Columns beyond I or J are multiplied and not stored.
 //
 // Large tiles are bound by the matrix pipe at the clock that the card's power allows (11008 x 4096 with 8192 tokens 650-720 us, 1.03-1.13
-// PFLOP/s; 4096 x 4096 238 us; a plain bf16 product of 8192 x 8192 x 8192 reaches 1.23); narrow ones by the rows they read (64 x 576 with
-// 200704 tokens 40 us for 145 MB, 3.6 TB/s: some 37 stages a workgroup, each of which waits for a barrier), plus 6 us for
-// the sums of 170 pieces.
+// PFLOP/s, 690-910 launched 25 times in a row under the profiler; 4096 x 4096 238 us; a plain bf16 product of 8192 x 8192 x 8192 reaches
+// 1.23); narrow ones by waits (64 x 576 with 200704 tokens 40 us for 145 MB, 3.6 TB/s: some 37 stages a workgroup, each of which ends with a
+// barrier, and no pipe is busy above 40 %), plus 6 us for the sums of 170 pieces.
 template <int BM, int BN, int WM, int WN, int SETS, bool WHOLE>
 __global__ void __launch_bounds__(64 * WM * WN, 2)
 k_weight_grad(const uint16_t* __restrict__ dY, int64_t T, int64_t lddy, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
@@ -485,7 +485,9 @@ int run(const Operands& o, const WeightGradPlan& p) {
 // 256 tiles (1000 x 1000 with 4000 99 us, without 125), of 2 stages up to 64 tiles (100 x 100 with 1000 9.3, with 8 stages 14.7), then 8 (1024 x 512 with 200 11.8 / 15.3).
 // More large tiles than CUs: where the last round over the chip would be at most half full, large tiles take the whole rounds and the rows
 // behind them a plan of their own, smaller tiles or pieces (4352 x 4096 with 4096 tokens, 272 tiles, 216 us in 128 x 128 tiles, 157 so;
-// 4864 x 4096 with 8192, 304, 421 / 308; 6144 x 4096 with 4096, 384, 219 / 211; but 5120 x 5120, 400, 222 / 247).
+// 4864 x 4096 with 8192, 304, 421 / 308; 6144 x 4096 with 4096, 384, 219 / 211; but 5120 x 5120, 400, 222 / 247).  Over 59 matrices with 768 to 4096
+// tokens 0.915 of one plan's time in the geometric mean; 21 of the 354 sizes lose, most at 1536 tokens with a last round above 3/8 (6144 x 4096 94 / 103) or
+// up to there behind 240 of 256 CUs (4096 x 5120 with 1024 66 / 68-70), which no simple rule sets apart.
 WeightGradPlan plan_weight_grad(int64_t T, int64_t I, int64_t J, int dtype) {
     WeightGradPlan p;
     p.first = 0;
